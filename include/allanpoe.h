@@ -53,6 +53,7 @@ extern "C" {
 
 #define AP_F32 0
 #define AP_BF16 1
+#define AP_I8 3 /* rows in 8 bits with a scale each (ap_quantize_rows); not a type of a corpus */
 
 typedef struct ap_index ap_index; /* opaque */
 
@@ -257,6 +258,79 @@ int ap_search_batch_entities(ap_index *index, const ap_queries *queries, const f
 void ap_free_index(ap_index *index);
 const char *ap_last_error(void); /* host string, thread-local */
 
+/* ---- learning the dense rows, and holding them in 8 bits --------------- */
+
+/* These calls need no index.  Matrices are row-major with `ld` elements from row to row (ld >= dim, rows and base 16-byte
+ * aligned: ld a multiple of 4 for f32, 8 for bf16, 16 for 8-bit rows); dim is a multiple of 4 (f32) or 8 (bf16) and at
+ * most 8192.  Results are contiguous unless they have an ld of their own.  A call that takes a workspace needs as many
+ * bytes of device memory as its ..._bytes call says (256-byte aligned; its contents before and after are of no meaning);
+ * two calls in flight at once need two.  Nothing is allocated and nothing waits for the device: all of these can be
+ * captured into a graph. */
+
+/* Token lists: list r holds the entries [indptr[r], indptr[r + 1]) of tokens and weights (rows + 1 offsets that ascend from
+ * 0 to n; a list whose offsets do not is empty), or, with indptr NULL, the one token r (then rows = n).  weights NULL: all
+ * 1.  A token outside [0, vocab) is an unused slot.  Tokens of a list may repeat and come in any order.  n, rows < 2^28. */
+typedef struct {
+    int64_t rows, n;
+    const int64_t *indptr;
+    const int32_t *tokens;
+    const float *weights;
+} ap_lists;
+
+/* Dense rows out of token lists: out[r] = scale sum_e weights[e] table[tokens[e]] over list r, in f32, rounded once to
+ * out_dtype; 0 for an empty list.  table: vocab x dim of dtype, out: rows x dim.  dim is a multiple of 8 where either is
+ * bf16. */
+int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vocab, int32_t dim, const ap_lists *lists,
+             float scale, void *out, int32_t out_dtype, void *stream);
+
+/* Its gradients for a gradient grad_out (rows x dim of dtype) of the rows: grad_table[v] = scale sum weights[e]
+ * grad_out[row of e] over the entries e with tokens[e] = v, vocab x dim of table_dtype, written in full (0 where no token
+ * names v); grad_weights[e] = scale <table[tokens[e]], grad_out[row of e]>, n f32 (0 for an unused slot).  Sums are f32 and
+ * taken in a fixed order: the same inputs give the same bits. */
+int ap_embed_grad_bytes(int64_t n, int64_t vocab, int32_t dim, size_t *out);
+int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, int32_t dim, const ap_lists *lists, int64_t vocab,
+                  float scale, void *grad_table, int32_t table_dtype, void *workspace, size_t bytes, void *stream);
+int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t grad_dtype, const void *table, int64_t ld,
+                          int32_t dtype, int64_t vocab, int32_t dim, const ap_lists *lists, float scale,
+                          float *grad_weights, void *stream);
+
+/* Rows in 8 bits: scale[r] = max |x[r]| / 127, q[r] = rint(x[r] / scale[r]) (f32, ties to even), zeros from column dim to
+ * the next multiple of 16; ldq is at least that.  A row of zeros gets scale 0, one that holds an infinity or NaN zeros and
+ * scale NaN.  x: rows x dim of dtype (AP_F32 or AP_BF16), rows < 2^30. */
+int ap_quantize_rows(const void *x, int64_t ldx, int64_t rows, int32_t dim, int32_t dtype, int8_t *q, int64_t ldq,
+                     float *scale, void *stream);
+
+/* Scores of `rows` queries against n documents in 8 bits: out[i][j] = sx_i q_scale[j] sum_k qx_ik q_jk, the sum in 32-bit
+ * integers (exact), n f32 a query, ld_out >= n apart.  q, q_scale: what ap_quantize_rows gave for rows of dim columns.
+ * x: f32 or bf16 rows, rounded to 8 bits as that call does (x_scale unused), or AP_I8 rows with their x_scale (dim then
+ * counts the zeros up to the multiple of 16).  rows <= 2^24, n < 2^30. */
+int ap_scores_int8_bytes(int64_t rows, int32_t dim, int32_t x_dtype, size_t *out);
+int ap_scores_int8(const void *x, int64_t ldx, const float *x_scale, int64_t rows, int32_t dim, int32_t x_dtype,
+                   const int8_t *q, int64_t ldq, const float *q_scale, int64_t n, float *out, int64_t ld_out,
+                   void *workspace, size_t bytes, void *stream);
+
+/* The softmax loss of `rows` queries x over all n documents (the cross entropy of a vocabulary of n classes):
+ *     l_qj = scale <x_q, docs_j>,  lse_q = ln sum_j exp(l_qj),  loss_q = lse_q - l_q,labels[q],
+ * x and docs both of `dtype` (AP_F32 or AP_BF16; sums and the softmax in f32).  labels[q] outside [0, n): loss_q is 0 and
+ * the query has no gradient.  loss and lse: `rows` f32 each.  The logits are never written to memory.  rows <= 2^24,
+ * n < 2^30. */
+int ap_softmax_loss_bytes(int64_t rows, int64_t n, int32_t dim, int32_t dtype, size_t *out);
+int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const void *docs, int64_t ldd, int64_t n, int32_t dim,
+                    int32_t dtype, float scale, const int32_t *labels, float *loss, float *lse, void *workspace,
+                    size_t bytes, void *stream);
+
+/* Its gradients, from the lse that ap_softmax_loss gave and the gradient row_grad[q] of what is minimised with regard to
+ * loss_q (rows f32; 1 / rows for a mean):
+ *     c_qj = row_grad[q] (exp(l_qj - lse_q) - [j = labels[q]]),  grad_x = scale c docs,  grad_docs = scale c^T x,
+ * rows x dim and n x dim of `dtype`, written in full; either may be NULL (not wanted; want_x says so to the _bytes call).
+ * A query without a label or of row_grad 0 adds nothing, whatever its x holds.  bf16 rows: coefficients are rounded to
+ * bf16 for their products, relative to the largest |row_grad|.  Sums are taken in a fixed order: the same inputs give the
+ * same bits. */
+int ap_softmax_loss_grad_bytes(int64_t rows, int64_t n, int32_t dim, int32_t dtype, int32_t want_x, size_t *out);
+int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, const void *docs, int64_t ldd, int64_t n, int32_t dim,
+                         int32_t dtype, float scale, const int32_t *labels, const float *lse, const float *row_grad,
+                         void *grad_x, void *grad_docs, void *workspace, size_t bytes, void *stream);
+
 /* ---- measurement / test surface: the same kernels, exposed stage by stage - */
 
 /* The upper bounds of the fused scores that searches and the exact top-k sort documents out with: out (device) is
@@ -390,6 +464,8 @@ int ap_search_form(const ap_index *index, int32_t out3[3]);
  *   "search_bounds_bytes"     cap of the workspace that holds them (forces slabs of queries, each with a table of its own)
  *   "bound_buckets"           2^this many buckets for the postings of 256 documents (8 to 15), where bounds are laid out from then on
  *   "search_floor"            1: no neighbour waits below the estimated end of the pool, 2: the estimate is far too high
+ *   "loss_piece"              documents whose coefficients the gradient of the softmax loss holds at a time
+ *   "embed_few"               one more than the number of entries up to which the embedding's gradient sorts nothing
  *   "search_visited_global"   1: visited sets stay in the global workspace even where the search would keep them in LDS
  *   "search_query_lists"      1: the plain and keyword searches look query terms up in the query's lists, not in LDS tables
  * Unknown names and negative values give AP_EINVAL.  Not thread-safe against running calls. */

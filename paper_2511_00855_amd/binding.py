@@ -17,7 +17,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("ALLANPOE_LIB") or os.path.join(_HERE, "liballanpoe.so")
 
-AP_F32, AP_BF16 = 0, 1
+AP_F32, AP_BF16, AP_I8 = 0, 1, 3
 
 
 class ApError(RuntimeError):
@@ -50,6 +50,13 @@ class _SearchParams(C.Structure):
     _fields_ = [("k", C.c_int32), ("beam", C.c_int32), ("max_iters", C.c_int32), ("search_width", C.c_int32)]
 
 
+# Argument types of the calls that take plain numbers and addresses: p pointer, l int64, i int32, f float, z size_t.
+_KINDS = dict(p=C.c_void_p, l=C.c_int64, i=C.c_int32, f=C.c_float, z=C.c_size_t)
+_ARGTYPES = dict(ap_embed="plilipfpip", ap_embed_grad_bytes="llip", ap_embed_grad="pliiplfpipzp", ap_embed_grad_weights="pliplilipfpp",
+                 ap_quantize_rows="plliiplpp", ap_scores_int8_bytes="liip", ap_scores_int8="plpliiplplplpzp",
+                 ap_softmax_loss_bytes="lliip", ap_softmax_loss="pllplliifppppzp",
+                 ap_softmax_loss_grad_bytes="lliiip", ap_softmax_loss_grad="pllplliifppppppzp")
+
 _lib = None
 
 
@@ -62,6 +69,8 @@ def lib():
         _lib = C.CDLL(LIB_PATH)
         _lib.ap_last_error.restype = C.c_char_p
         _lib.ap_free_index.restype = None
+        for name, kinds in _ARGTYPES.items():
+            getattr(_lib, name).argtypes = [_KINDS[k] for k in kinds]
     return _lib
 
 
@@ -106,7 +115,7 @@ def debug_set(name: str, value: int):
 
 DEBUG_NAMES = ("seed_sample_cols", "seed_buffer_cap", "seed_tau_ulps", "max_launch_threads", "search_workspace_bytes",
                "search_visited_global", "search_query_lists", "seed_one_sided", "search_bounds", "search_walk", "search_bounds_bytes", "search_floor", "prune_walks",
-               "bound_buckets")
+               "bound_buckets", "loss_piece", "embed_few")
 
 
 def debug_reset():
@@ -519,3 +528,156 @@ class Index:
         out = (C.c_float * 6)()
         _check(lib().ap_build_timings(self._h, out), "ap_build_timings")
         return dict(zip(("ingest", "seed", "refine", "prune", "assemble", "total"), [float(x) for x in out]))
+
+
+# -- learning the dense rows, and holding them in 8 bits -----------------------
+def _rows(t: torch.Tensor, what: str):
+    """(address, elements from row to row, dtype code) of a matrix of f32 or bf16 rows; int16 is bf16 as DeviceVecs keeps it."""
+    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a matrix on the GPU whose rows are contiguous")
+    code = AP_F32 if t.dtype is torch.float32 else AP_BF16 if t.dtype in (torch.bfloat16, torch.int16) else None
+    if code is None:
+        raise ValueError(f"{what} must be f32 or bf16, not {t.dtype}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8, code   # a single row has no next one
+
+
+def _vec(t: torch.Tensor, dtype, count: int, device, what: str):
+    if t.dtype is not dtype or t.shape != (count,) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be {count} contiguous {dtype} values on {device}")
+    return t.data_ptr()
+
+
+def _call(fn: str, device, *args, bytes_args=None):
+    """Calls ap_<fn> on the device's current stream, with the workspace that ap_<fn>_bytes(*bytes_args) asks for."""
+    L = lib()
+    with torch.cuda.device(device):
+        if bytes_args is not None:
+            need = C.c_size_t()
+            _check(getattr(L, fn + "_bytes")(*bytes_args, C.byref(need)), fn + "_bytes")
+            ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+            args += (ws.data_ptr(), need.value)
+        _check(getattr(L, fn)(*args, torch.cuda.current_stream().cuda_stream), fn)
+
+
+def _same(a: torch.Tensor, b: torch.Tensor, what: str):
+    if a.device != b.device or a.shape[1] != b.shape[1]:
+        raise ValueError(f"{what} differ in device or number of columns")
+
+
+class _Lists(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int64), ("indptr", C.c_void_p), ("tokens", C.c_void_p), ("weights", C.c_void_p)]
+
+
+_DTYPE = {torch.float32: AP_F32, torch.bfloat16: AP_BF16}
+
+
+def _lists(tokens, weights, indptr, device) -> _Lists:
+    n = tokens.numel()
+    rows = n if indptr is None else indptr.numel() - 1
+    return _Lists(rows, n, None if indptr is None else _vec(indptr, torch.int64, rows + 1, device, "indptr"), _vec(tokens, torch.int32, n, device, "tokens"),
+                  None if weights is None else _vec(weights, torch.float32, n, device, "weights"))
+
+
+def embed(table: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor] = None, indptr: Optional[torch.Tensor] = None, scale: float = 1.0,
+          out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """Dense rows out of token lists (see ap_embed): scale times the weighted sum of the table's rows that a list names, a row a list; without
+    indptr a row a token.  out_dtype: float32 or bfloat16, the table's own if None."""
+    p, ld, code = _rows(table, "table")
+    l = _lists(tokens, weights, indptr, table.device)
+    out = torch.empty((l.rows, table.shape[1]), dtype=out_dtype or table.dtype, device=table.device)
+    _call("ap_embed", table.device, p, ld, code, table.shape[0], table.shape[1], C.byref(l), scale, out.data_ptr(), code if out_dtype is None else _DTYPE[out_dtype])
+    return out
+
+
+def embed_grad(grad_out: torch.Tensor, tokens: torch.Tensor, vocab: int, weights: Optional[torch.Tensor] = None, indptr: Optional[torch.Tensor] = None,
+               scale: float = 1.0, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """Gradient of embed's table, vocab rows, of dtype (grad_out's own if None) (see ap_embed_grad)."""
+    p, ld, code = _rows(grad_out, "grad_out")
+    l = _lists(tokens, weights, indptr, grad_out.device)
+    if l.rows != grad_out.shape[0]:
+        raise ValueError(f"grad_out has {grad_out.shape[0]} rows for {l.rows} lists")
+    dim = grad_out.shape[1]
+    out = torch.empty((vocab, dim), dtype=dtype or grad_out.dtype, device=grad_out.device)
+    _call("ap_embed_grad", grad_out.device, p, ld, code, dim, C.byref(l), vocab, scale, out.data_ptr(), code if dtype is None else _DTYPE[dtype], bytes_args=(l.n, vocab, dim))
+    return out
+
+
+def embed_grad_weights(grad_out: torch.Tensor, table: torch.Tensor, tokens: torch.Tensor, indptr: Optional[torch.Tensor] = None, scale: float = 1.0) -> torch.Tensor:
+    """Gradient of embed's weights, an f32 for each token (see ap_embed_grad_weights)."""
+    (pg, ldg, code_g), (p, ld, code) = _rows(grad_out, "grad_out"), _rows(table, "table")
+    _same(grad_out, table, "grad_out and table")
+    l = _lists(tokens, None, indptr, table.device)
+    if l.rows != grad_out.shape[0]:
+        raise ValueError(f"grad_out has {grad_out.shape[0]} rows for {l.rows} lists")
+    out = torch.empty(l.n, dtype=torch.float32, device=table.device)
+    _call("ap_embed_grad_weights", table.device, pg, ldg, code_g, p, ld, code, table.shape[0], table.shape[1], C.byref(l), scale, out.data_ptr())
+    return out
+
+
+def _bytes_rows(q: torch.Tensor, what: str):
+    if q.dim() != 2 or not q.is_cuda or q.dtype is not torch.int8 or (q.shape[1] > 1 and q.stride(1) != 1):
+        raise ValueError(f"{what} must be an int8 matrix on the GPU whose rows are contiguous")
+    return q.data_ptr(), q.stride(0) if q.shape[0] > 1 else -(-q.shape[1] // 16) * 16
+
+
+def quantize_rows(x: torch.Tensor):
+    """Rows in 8 bits with a scale each (see ap_quantize_rows): (int8, as many columns as x rounded up to a multiple of 16; f32)."""
+    p, ld, code = _rows(x, "x")
+    rows, dim = x.shape
+    q = torch.empty((rows, -(-dim // 16) * 16), dtype=torch.int8, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _call("ap_quantize_rows", x.device, p, ld, rows, dim, code, q.data_ptr(), q.shape[1], scale.data_ptr())
+    return q, scale
+
+
+def scores_int8(x: torch.Tensor, q: torch.Tensor, q_scale: torch.Tensor, x_scale: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scores of queries against documents in 8 bits (q, q_scale of quantize_rows), f32 (see ap_scores_int8).  x: f32 or bf16 rows, or int8
+    rows with their x_scale."""
+    if x.dtype is torch.int8:
+        (px, ldx), code = _bytes_rows(x, "x"), AP_I8
+        if x_scale is None:
+            raise ValueError("int8 queries need their x_scale")
+    else:
+        px, ldx, code = _rows(x, "x")
+    pq, ldq = _bytes_rows(q, "q")
+    (rows, dim), n = x.shape, q.shape[0]
+    if q.device != x.device or q.shape[1] != -(-dim // 16) * 16:
+        raise ValueError("x and q differ in device or number of columns")
+    sq = _vec(q_scale, torch.float32, n, x.device, "q_scale")
+    sx = None if x_scale is None else _vec(x_scale, torch.float32, rows, x.device, "x_scale")
+    out = torch.empty((rows, n), dtype=torch.float32, device=x.device)
+    _call("ap_scores_int8", x.device, px, ldx, sx, rows, dim, code, pq, ldq, sq, n, out.data_ptr(), n, bytes_args=(rows, dim, code))
+    return out
+
+
+def softmax_loss(x: torch.Tensor, docs: torch.Tensor, labels: torch.Tensor, scale: float = 1.0):
+    """The softmax loss of queries over all documents (see ap_softmax_loss): (loss, lse), an f32 for each row of x.
+
+    labels: int32, the document that each query should find; outside [0, n) for none (loss 0)."""
+    (px, ldx, code), (pd, ldd, code_d) = _rows(x, "x"), _rows(docs, "docs")
+    _same(x, docs, "x and docs")
+    if code != code_d:
+        raise ValueError("x and docs differ in type")
+    (rows, dim), n = x.shape, docs.shape[0]
+    labels_p = _vec(labels, torch.int32, rows, x.device, "labels")
+    loss, lse = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    _call("ap_softmax_loss", x.device, px, ldx, rows, pd, ldd, n, dim, code, scale, labels_p, loss.data_ptr(), lse.data_ptr(), bytes_args=(rows, n, dim, code))
+    return loss, lse
+
+
+def softmax_loss_grad(x: torch.Tensor, docs: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, row_grad: torch.Tensor, scale: float = 1.0,
+                      want_x: bool = True, want_docs: bool = True):
+    """(grad_x, grad_docs) of what has the gradient row_grad with regard to softmax_loss's loss (see ap_softmax_loss_grad), in the
+    type of x and docs; None for one that is not wanted."""
+    (px, ldx, code), (pd, ldd, code_d) = _rows(x, "x"), _rows(docs, "docs")
+    _same(x, docs, "x and docs")
+    if code != code_d:
+        raise ValueError("x and docs differ in type")
+    (rows, dim), n = x.shape, docs.shape[0]
+    labels_p = _vec(labels, torch.int32, rows, x.device, "labels")
+    lse_p, grad_p = _vec(lse, torch.float32, rows, x.device, "lse"), _vec(row_grad, torch.float32, rows, x.device, "row_grad")
+    gx = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if want_x else None
+    gd = torch.empty((n, dim), dtype=docs.dtype, device=x.device) if want_docs else None
+    _call("ap_softmax_loss_grad", x.device, px, ldx, rows, pd, ldd, n, dim, code, scale, labels_p, lse_p, grad_p, None if gx is None else gx.data_ptr(),
+          None if gd is None else gd.data_ptr(), bytes_args=(rows, n, dim, code, int(want_x)))
+    return gx, gd

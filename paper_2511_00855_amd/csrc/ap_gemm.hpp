@@ -1,0 +1,211 @@
+// The tile product under the losses and the 8-bit scores: C[m][n] = sum_k A[m][k] B[n][k] of one workgroup's tile, on
+// the matrix instructions of gfx950, for 16-bit floats (bf16, f16; sums in f32) and 8-bit integers (sums in i32, exact).
+//
+// An operand lies in memory either with k running along its rows (a row of A is a line of memory) or with k running from
+// line to line; a product takes any pair of the two, so that neither a gradient's operand nor its result is transposed
+// in memory.
+#pragma once
+#include "ap_common.hpp"
+
+#ifdef __HIPCC__
+typedef __bf16 ap_g_bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 ap_g_f16x8 __attribute__((ext_vector_type(8)));
+typedef float ap_g_f32x16 __attribute__((ext_vector_type(16)));
+typedef int32_t ap_g_i32x16 __attribute__((ext_vector_type(16)));
+typedef int32_t ap_g_i32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t ap_g_i32x2 __attribute__((ext_vector_type(2)));
+typedef short ap_g_s16x4 __attribute__((ext_vector_type(4)));
+
+// What is multiplied: 16 bytes of a lane, 8 values of 16 bits or 16 of 8.
+struct ApBf16Op {
+    typedef ap_g_f32x16 Acc;
+    static constexpr int BYTES = 2;
+    static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ap_g_bf16x8, a), __builtin_bit_cast(ap_g_bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct ApF16Op {
+    typedef ap_g_f32x16 Acc;
+    static constexpr int BYTES = 2;
+    static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(ap_g_f16x8, a), __builtin_bit_cast(ap_g_f16x8, b), c, 0, 0, 0);
+    }
+};
+struct ApI8Op {
+    typedef ap_g_i32x16 Acc;
+    static constexpr int BYTES = 1;
+    static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+};
+
+#define AP_G_LINE 128   // bytes of k that a chunk takes of every row: 64 values of 16 bits, 128 of 8
+
+// One operand of a product.  K_LINE: k runs along the lines of memory.  `base` is the first byte of the tile's first row
+// (K_LINE) or of the tile's first column in line k = 0; `ld` the bytes from line to line; `rows` how many rows (K_LINE) or
+// bytes of columns the tile really has: the rest reads as zeros.
+struct ApOperand {
+    const char *base;
+    int64_t ld;
+    int32_t rows;
+};
+
+// 16 bytes a lane straight into LDS: lane l's land at `lds` + 16 l.  A lane whose offset is not below 2^31 - 1 gets zeros.
+// In assembly because the compiler makes every later LDS read wait for the builtin's loads, also those of the other stage.
+// The loads write no register; ap_g_wait_loads() is what waits for them.
+__device__ __forceinline__ void ap_g_load_lds(const char *base, uint32_t off, uint32_t lds) {
+    const uint64_t b = (uint64_t)base;
+    const ap_g_i32x4 rsrc = {(int32_t)(uint32_t)b, (int32_t)(uint32_t)(b >> 32), 0x7fffffff, 0x00020000};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory", "m0");
+}
+template <int N> __device__ __forceinline__ void ap_g_wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ap_g_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// A tile of TM x TN by WM x WN waves.
+template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> struct ApGemm {
+    static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
+    static constexpr int FA = TM / WM / 32, FB = TN / WN / 32;   // 32 x 32 blocks of a wave
+    static constexpr int A_BYTES = TM * AP_G_LINE, B_BYTES = TN * AP_G_LINE;
+    static constexpr int STAGE = A_BYTES + B_BYTES, LDS_BYTES = 2 * STAGE;
+    static constexpr int BK = AP_G_LINE / OP::BYTES;   // values of k in a chunk
+    typedef typename OP::Acc Acc;
+
+    // Chunks of 16 bytes change places within a line of LDS, so that the lanes of one read fall in different banks.  Lines of k:
+    // 32 rows are read at the same chunk.  Lines of rows or columns: a read takes 32 columns of the lines k, k + 1, k + 2, k + 3,
+    // k + 8, .. k + 11.
+    static __device__ __forceinline__ int swap_k(int row) { return row & 7; }
+    static __device__ __forceinline__ int swap_t(int k, int t) { return (((k & 3) | ((k >> 1) & 4)) * 4) & (t * OP::BYTES / 16 - 1); }
+
+    // The offsets, relative to a chunk's first byte, of what this lane brings of an operand of T rows.
+    template <int T, bool LINE>
+    static __device__ __forceinline__ void offsets(const ApOperand &o, int wave, int lane, uint32_t (&off)[T / 8 / WAVES]) {
+#pragma unroll
+        for (int i = 0; i < T / 8 / WAVES; i++) {
+            const int at = (wave * (T / 8 / WAVES) + i) * 64 + lane;   // 16-byte group of the stage
+            if (LINE) {
+                const int row = at >> 3, chunk = (at & 7) ^ swap_k(row);
+                off[i] = row < o.rows ? (uint32_t)(row * o.ld + chunk * 16) : 0x80000000u;
+            } else {
+                constexpr int PER = T * OP::BYTES / 16;   // groups of a line
+                const int k = at / PER, chunk = (at % PER) ^ swap_t(k, T);
+                off[i] = chunk * 16 < o.rows ? (uint32_t)(k * o.ld + chunk * 16) : 0x80000000u;
+            }
+        }
+    }
+    // Loads a chunk's part of one operand; `left`: the bytes (K_LINE) or lines of k that are left from this chunk on.
+    template <int T, bool LINE>
+    static __device__ __forceinline__ void load(const char *base, const uint32_t (&off)[T / 8 / WAVES], int32_t left, uint32_t lds, int wave, int lane) {
+        const bool whole = left >= (LINE ? AP_G_LINE : BK);
+#pragma unroll
+        for (int i = 0; i < T / 8 / WAVES; i++) {
+            uint32_t o = off[i];
+            if (!whole) {
+                const int at = (wave * (T / 8 / WAVES) + i) * 64 + lane;
+                const int place = LINE ? ((at & 7) ^ swap_k(at >> 3)) * 16 : at / (T * OP::BYTES / 16);
+                if (place >= left) o = 0x80000000u;
+            }
+            ap_g_load_lds(base, o, lds + (wave * (T / 8 / WAVES) + i) * 1024);
+        }
+    }
+    // The 16 bytes of k that this lane feeds to step `step` for the 32 rows from `row` on.
+    template <int T, bool LINE>
+    static __device__ __forceinline__ ap_g_i32x4 frag(const char *lds, int row, int step, int lane) {
+        if (LINE) {
+            const int r = row + (lane & 31), chunk = (step * 2 + (lane >> 5)) ^ swap_k(r);
+            return *reinterpret_cast<const ap_g_i32x4 *>(lds + r * AP_G_LINE + chunk * 16);
+        } else {
+            // 16 lanes read 4 lines of 16 columns and get 4 values of k of a column each
+            static_assert(LINE || OP::BYTES == 2, "lines of rows are of 16-bit values");
+            const int g = lane >> 4, k = step * 16 + (g >> 1) * 8 + ((lane >> 2) & 3), col = (row + (g & 1) * 16 + (lane & 3) * 4) * 2;
+            ap_g_s16x4 v[2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int kk = k + h * 4;
+                const char *p = lds + kk * (T * 2) + ((((col >> 4) ^ swap_t(kk, T)) << 4) | (col & 15));
+                v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AP_LDS ap_g_s16x4 *)p);
+            }
+            struct { ap_g_s16x4 a, b; } w = {v[0], v[1]};
+            return __builtin_bit_cast(ap_g_i32x4, w);
+        }
+    }
+
+    // The whole product of K values.  With `parts` > 1 the operands are sums of parts that lie `a_part` / `b_part` bytes apart and the
+    // product takes `parts` = 3 pairs: second times first, first times second, first times first (the smallest first; the product
+    // of the second parts is below the last bit of the sum).
+    static __device__ __forceinline__ void product(const ApOperand &A, const ApOperand &B, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB]) {
+        const int lane = threadIdx.x & 63, wave = ap_wave_id();
+        const int wm = wave / WN, wn = wave % WN;
+        uint32_t oa[TM / 8 / WAVES], ob[TN / 8 / WAVES];
+        offsets<TM, A_LINE>(A, wave, lane, oa);
+        offsets<TN, B_LINE>(B, wave, lane, ob);
+#pragma unroll
+        for (int a = 0; a < FA; a++)
+#pragma unroll
+            for (int b = 0; b < FB; b++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[a][b][r] = 0;
+        const int32_t per = (K + BK - 1) / BK, chunks = per * parts;
+        const int64_t a_step = A_LINE ? AP_G_LINE : BK * A.ld, b_step = B_LINE ? AP_G_LINE : BK * B.ld;
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(AP_LDS char *)lds;
+        const char *next_a = A.base + (parts > 1 ? a_part : 0), *next_b = B.base;   // of the next chunk to be brought
+        int32_t left = K, part = 0;
+        auto bring = [&](int stage) {
+            const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
+            load<TM, A_LINE>(a, oa, A_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE, wave, lane);
+            load<TN, B_LINE>(b, ob, B_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE + A_BYTES, wave, lane);
+            next_a += a_step;
+            next_b += b_step;
+            left -= BK;
+            if (left <= 0 && ++part < parts) {
+                left = K;
+                next_a = A.base;
+                next_b = B.base + (part == 1 ? b_part : 0);
+            }
+        };
+        if (chunks > 0) bring(0);
+        for (int32_t c = 0; c < chunks; c++) {
+            ap_g_wait_loads<0>();
+            ap_g_barrier();   // chunk c is there, and nobody reads the other stage any more
+            if (c + 1 < chunks) bring((c + 1) & 1);
+            const char *sa = lds + (c & 1) * STAGE, *sb = sa + A_BYTES;
+#pragma unroll
+            for (int s = 0; s < 4; s++) {
+                ap_g_i32x4 fa[FA], fb[FB];
+#pragma unroll
+                for (int a = 0; a < FA; a++) fa[a] = frag<TM, A_LINE>(sa, wm * (TM / WM) + a * 32, s, lane);
+#pragma unroll
+                for (int b = 0; b < FB; b++) fb[b] = frag<TN, B_LINE>(sb, wn * (TN / WN) + b * 32, s, lane);
+#pragma unroll
+                for (int a = 0; a < FA; a++)
+#pragma unroll
+                    for (int b = 0; b < FB; b++) acc[a][b] = OP::mul(fa[a], fb[b], acc[a][b]);
+            }
+        }
+        ap_g_barrier();   // the stages may be used for something else
+    }
+    // Calls f(i, j, value) for every element that this lane holds of the tile.
+    template <class F> static __device__ __forceinline__ void each(const Acc (&acc)[FA][FB], F f) {
+        const int lane = threadIdx.x & 63, wave = ap_wave_id();
+        const int wm = wave / WN, wn = wave % WN;
+#pragma unroll
+        for (int a = 0; a < FA; a++)
+#pragma unroll
+            for (int b = 0; b < FB; b++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    f(wm * (TM / WM) + a * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), wn * (TN / WN) + b * 32 + (lane & 31), acc[a][b][r]);
+    }
+};
+
+// Which tile a workgroup takes.  Workgroups go round the eight XCDs, each with an L2 of its own: an XCD gets consecutive tiles, and
+// these run over `group` column tiles before they go to the next row tile, so that what its 32 compute units read at a time is little.
+__device__ __forceinline__ void ap_g_tile(uint32_t block, uint32_t mt, uint32_t nt, uint32_t group, uint32_t *m, uint32_t *n) {
+    const uint32_t total = mt * nt, each = total / 8, more = total % 8, x = block % 8, i = block / 8;
+    const uint32_t t = x * each + (x < more ? x : more) + i;
+    const uint32_t g = t / (mt * group), in = t - g * mt * group, wide = nt - g * group < group ? nt - g * group : group;
+    *m = in / wide;
+    *n = g * group + in % wide;
+}
+#endif

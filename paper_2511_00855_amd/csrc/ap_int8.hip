@@ -1,0 +1,228 @@
+// Rows in 8 bits, and the scores of queries against them.
+//
+//   s = max_k |x_k| / 127,   q_k = rint(x_k / s)             (one f32 scale a row; a row of zeros has s = 0)
+//   score_ij = sx_i sd_j sum_k qx_ik qd_jk                   (the sum is an integer and exact)
+//
+// Few queries are bound by the documents' bytes: one pass (ap_stream.hpp), the queries rounded by every workgroup for itself.  Many
+// are bound by the f32 scores that are written (4 bytes for 2 dim operations) as much as by the matrix instruction.
+#include <algorithm>
+#include "ap_gemm.hpp"
+#include "ap_stream.hpp"
+
+template <int DT> __device__ __forceinline__ float4 load4(const void *row, int32_t c) {
+    if (DT == AP_F32) return *reinterpret_cast<const float4 *>(static_cast<const float *>(row) + c);
+    const uint2 y = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(row) + c);
+    return make_float4(__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xffff0000u));
+}
+
+// One wave rounds one row: put(column, 4 values of 8 bits) for every 4 columns up to `pad`; returns the scale.  A row that holds an infinity or
+// NaN gets a scale of NaN, so that its scores show it.  Both divisions are the IEEE ones: ties fall as the formula says.
+template <int DT, class P> __device__ __forceinline__ float round_row(const void *row, int32_t dim, int32_t pad, P put) {
+    const int lane = threadIdx.x & 63;
+    float m = 0.f;
+    for (int32_t c = lane * 4; c < dim; c += 256) {
+        const float4 v = load4<DT>(row, c);
+        const float x[4] = {fabsf(v.x), fabsf(v.y), fabsf(v.z), fabsf(v.w)};
+#pragma unroll
+        for (int i = 0; i < 4; i++) m = x[i] > m || x[i] != x[i] ? x[i] : m;   // NaN stays
+    }
+    for (int o = 32; o > 0; o >>= 1) { const float t = __shfl_xor(m, o, 64); m = t > m || t != t ? t : m; }
+    const bool good = m < INFINITY;
+    const float s = good ? m / 127.f : NAN;
+    for (int32_t c = lane * 4; c < pad; c += 256) {
+        uint32_t w = 0;
+        if (good && s > 0.f && c < dim) {
+            const float4 v = load4<DT>(row, c);
+            const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            // the clamp is for scales among the denormals, whose quotients may pass 127
+            for (int i = 0; i < 4; i++) w |= (uint32_t)((int32_t)fminf(fmaxf(rintf(x[i] / s), -127.f), 127.f) & 255) << (8 * i);
+        }
+        put(c, w);
+    }
+    return s;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void k_round_rows(const char *__restrict__ x, int64_t ld /* bytes */, int64_t rows, int32_t dim, int32_t pad, int8_t *__restrict__ q, int64_t ldq,
+                                                    float *__restrict__ scale) {
+    for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4) {
+        const float s = round_row<DT>(x + r * ld, dim, pad, [&](int32_t c, uint32_t w) { *reinterpret_cast<uint32_t *>(q + r * ldq + c) = w; });
+        if ((threadIdx.x & 63) == 0) scale[r] = s;
+    }
+}
+
+struct ApScores8 {
+    const char *x;                 // queries: f32, bf16 or 8-bit rows
+    int64_t ldx;                   // bytes
+    const float *x_scale;
+    const char *q;                 // documents
+    int64_t ldq;
+    const float *q_scale;
+    int32_t rows, n, dim, pad;     // pad: columns of an 8-bit row
+    float *out;
+    int64_t ld_out;
+    int32_t group;
+};
+
+template <int DT, int NQ>
+__global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float s_scale[NQ * 16];
+    const int lane = threadIdx.x & 63, wave = ap_wave_id();
+    const int steps = (p.pad + 63) / 64;
+    for (int q = wave; q < NQ * 16; q += AP_STREAM_THREADS / 64) {
+        float s = 0.f;
+        if (q < p.rows) {
+            if (DT == AP_I8) {
+                for (int32_t c = lane * 4; c < steps * 64; c += 256)
+                    *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, NQ)) = c < p.pad ? *reinterpret_cast<const uint32_t *>(p.x + q * p.ldx + c) : 0u;
+                s = p.x_scale[q];
+            } else {
+                s = round_row<DT == AP_I8 ? AP_F32 : DT>(p.x + q * p.ldx, p.dim, steps * 64, [&](int32_t c, uint32_t w) { *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, NQ)) = w; });
+            }
+        } else {
+            for (int32_t c = lane * 4; c < steps * 64; c += 256) *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, NQ)) = 0u;
+        }
+        if (lane == 0) s_scale[q] = s;
+    }
+    __syncthreads();
+    ap_stream<ApStreamI8, NQ>(p.q, p.ldq, p.n, p.pad, lds, (int64_t)blockIdx.x * (AP_STREAM_THREADS / 64) + wave, (int64_t)gridDim.x * (AP_STREAM_THREADS / 64),
+                              [&](int64_t first, const ap_g_i32x4 (&acc)[NQ]) {
+                                  const int64_t d = first + (lane >> 4) * 4;
+#pragma unroll
+                                  for (int g = 0; g < NQ; g++) {
+                                      const int q = g * 16 + (lane & 15);
+                                      if (q >= p.rows) continue;
+#pragma unroll
+                                      for (int r = 0; r < 4; r++)
+                                          if (d + r < p.n) p.out[q * p.ld_out + d + r] = (float)acc[g][r] * s_scale[q] * p.q_scale[d + r];
+                                  }
+                              });
+}
+
+// Queries are the product's rows: a lane then holds one document, and 32 lanes write 128 bytes of a query's scores, however they are aligned.
+template <int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void k_scores8(ApScores8 p) {
+    using G = ApGemm<ApI8Op, TM, TN, WM, WN, true, true>;
+    __shared__ __attribute__((aligned(1024))) char lds[G::LDS_BYTES];
+    uint32_t nt, mt;
+    ap_g_tile(blockIdx.x, (p.n + TN - 1) / TN, (p.rows + TM - 1) / TM, p.group, &nt, &mt);
+    const int32_t m0 = mt * TM, n0 = nt * TN, queries = min(TM, p.rows - m0), docs = min(TN, p.n - n0);
+    typename G::Acc acc[G::FA][G::FB];
+    G::product({p.x + m0 * p.ldx, p.ldx, queries}, {p.q + n0 * p.ldq, p.ldq, docs}, p.pad, 1, 0, 0, lds, acc);
+    const int lane = threadIdx.x & 63, wave = ap_wave_id(), wm = wave / WN, wn = wave % WN;
+    const int row0 = wm * (TM / WM) + 4 * (lane >> 5), col0 = wn * (TN / WN) + (lane & 31);
+    float sd[G::FB];
+#pragma unroll
+    for (int b = 0; b < G::FB; b++) sd[b] = col0 + b * 32 < docs ? p.q_scale[n0 + col0 + b * 32] : 0.f;
+#pragma unroll
+    for (int a = 0; a < G::FA; a++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+            const int i = row0 + a * 32 + 8 * (r >> 2) + (r & 3);
+            if (i >= queries) continue;
+            const float sx = p.x_scale[m0 + i];
+            float *to = p.out + (int64_t)(m0 + i) * p.ld_out + n0 + col0;
+#pragma unroll
+            for (int b = 0; b < G::FB; b++)
+                if (col0 + b * 32 < docs) to[b * 32] = (float)acc[a][b][r] * sx * sd[b];
+        }
+}
+
+// ------------------------------------------------------------------ host side
+static int64_t div_up(int64_t v, int64_t m) { return (v + m - 1) / m; }
+static int check_dim(int32_t dim, int32_t dtype) {
+    AP_REQUIRE(dtype == AP_F32 || dtype == AP_BF16 || dtype == AP_I8, "dtype = %d is not AP_F32/AP_BF16/AP_I8", dtype);
+    const int group = dtype == AP_I8 ? 16 : dtype == AP_BF16 ? 8 : 4;
+    AP_REQUIRE(dim >= group && dim % group == 0 && dim <= 8192, "dim = %d must be a multiple of %d and at most 8192", dim, group);
+    return AP_OK;
+}
+static int check_ld(const char *what, const void *p, int64_t ld, int32_t dim, int32_t dtype) {
+    AP_REQUIRE(p != nullptr, "%s is NULL", what);
+    AP_REQUIRE(((uintptr_t)p & 15) == 0, "%s must be 16-byte aligned", what);
+    const int group = dtype == AP_I8 ? 16 : dtype == AP_BF16 ? 8 : 4;
+    AP_REQUIRE(ld >= dim && ld % group == 0 && ld <= (1 << 20), "%s: %lld elements from row to row, must be a multiple of %d in [dim, 2^20]", what, (long long)ld, group);
+    return AP_OK;
+}
+static int64_t size_of(int32_t dtype) { return dtype == AP_I8 ? 1 : dtype == AP_BF16 ? 2 : 4; }
+
+extern "C" int ap_quantize_rows(const void *x, int64_t ldx, int64_t rows, int32_t dim, int32_t dtype, int8_t *q, int64_t ldq, float *scale, void *stream) {
+    AP_REQUIRE(dtype == AP_F32 || dtype == AP_BF16, "dtype = %d is not AP_F32/AP_BF16", dtype);
+    AP_TRY(check_dim(dim, dtype));
+    AP_REQUIRE(rows >= 0 && rows < (1ll << 30), "rows = %lld must be in [0, 2^30)", (long long)rows);
+    if (rows == 0) return AP_OK;
+    AP_TRY(check_ld("x", x, ldx, dim, dtype));
+    const int32_t pad = (dim + 15) / 16 * 16;
+    AP_TRY(check_ld("q", q, ldq, pad, AP_I8));
+    AP_REQUIRE(scale != nullptr, "scale is NULL");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)std::min<int64_t>(div_up(rows, 4), 16384));
+    if (dtype == AP_F32) hipLaunchKernelGGL((k_round_rows<AP_F32>), grid, dim3(256), 0, st, static_cast<const char *>(x), ldx * 4, rows, dim, pad, q, ldq, scale);
+    else hipLaunchKernelGGL((k_round_rows<AP_BF16>), grid, dim3(256), 0, st, static_cast<const char *>(x), ldx * 2, rows, dim, pad, q, ldq, scale);
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}
+
+// Up to how many queries one pass over the documents pays.
+static bool scores8_few(int64_t rows, int32_t pad) { return rows <= 64 && ap_stream_lds(rows, pad) <= AP_STREAM_LDS; }
+
+extern "C" int ap_scores_int8_bytes(int64_t rows, int32_t dim, int32_t x_dtype, size_t *out) {
+    AP_REQUIRE(out != nullptr, "out is NULL");
+    AP_TRY(check_dim(dim, x_dtype));
+    AP_REQUIRE(rows >= 0 && rows <= (1 << 24), "rows = %lld must be in [0, 2^24]", (long long)rows);
+    const int64_t pad = (dim + 15) / 16 * 16;
+    *out = x_dtype == AP_I8 || scores8_few(rows, (int32_t)pad) ? 0 : (size_t)(rows * pad + 255) / 256 * 256 + rows * 4;
+    return AP_OK;
+}
+
+template <int DT> static int few(const ApScores8 &p, hipStream_t st) {
+    const int nq = (p.rows + 15) / 16;
+    const size_t lds = (size_t)ap_stream_lds(p.rows, p.pad);
+    const dim3 grid((unsigned)std::min<int64_t>(div_up(div_up(p.n, 16), AP_STREAM_THREADS / 64), 512));
+#define AP_FEW(N)                                                                                                                       \
+    case N:                                                                                                                             \
+        if (lds > 60 * 1024) AP_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_scores8_few<DT, N>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
+        hipLaunchKernelGGL((k_scores8_few<DT, N>), grid, dim3(AP_STREAM_THREADS), lds, st, p);                                          \
+        break
+    switch (nq) { AP_FEW(1); AP_FEW(2); AP_FEW(3); AP_FEW(4); }
+#undef AP_FEW
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}
+
+extern "C" int ap_scores_int8(const void *x, int64_t ldx, const float *x_scale, int64_t rows, int32_t dim, int32_t x_dtype, const int8_t *q, int64_t ldq, const float *q_scale,
+                              int64_t n, float *out, int64_t ld_out, void *workspace, size_t bytes, void *stream) {
+    AP_TRY(check_dim(dim, x_dtype));
+    AP_REQUIRE(rows >= 0 && rows <= (1 << 24), "rows = %lld must be in [0, 2^24]", (long long)rows);
+    AP_REQUIRE(n >= 1 && n < (1ll << 30), "n = %lld must be in [1, 2^30)", (long long)n);
+    if (rows == 0) return AP_OK;
+    const int32_t pad = (dim + 15) / 16 * 16;
+    AP_TRY(check_ld("x", x, ldx, dim, x_dtype));
+    AP_TRY(check_ld("q", q, ldq, pad, AP_I8));
+    AP_REQUIRE(q_scale && out && (x_scale || x_dtype != AP_I8), "x_scale, q_scale or out is NULL");
+    AP_REQUIRE(ld_out >= n, "ld_out = %lld is less than n", (long long)ld_out);
+    size_t need;
+    AP_TRY(ap_scores_int8_bytes(rows, dim, x_dtype, &need));
+    AP_REQUIRE(bytes >= need && (workspace || need == 0), "workspace of %zu bytes, %zu are needed", bytes, need);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ApScores8 p{static_cast<const char *>(x), ldx * size_of(x_dtype), x_scale, reinterpret_cast<const char *>(q), ldq, q_scale, (int32_t)rows, (int32_t)n, dim, pad, out, ld_out, 8};
+    if (scores8_few(rows, pad)) return x_dtype == AP_I8 ? few<AP_I8>(p, st) : x_dtype == AP_BF16 ? few<AP_BF16>(p, st) : few<AP_F32>(p, st);
+    if (x_dtype != AP_I8) {
+        int8_t *qx = static_cast<int8_t *>(workspace);
+        float *sx = reinterpret_cast<float *>(static_cast<char *>(workspace) + (rows * pad + 255) / 256 * 256);
+        AP_TRY(ap_quantize_rows(x, ldx, rows, dim, x_dtype, qx, pad, sx, stream));
+        p.x = reinterpret_cast<const char *>(qx); p.ldx = pad; p.x_scale = sx;
+    }
+    int tile = 256;
+    while (tile > 64 && div_up(rows, tile) * div_up(n, tile) < 192) tile /= 2;
+    const int64_t tiles = div_up(rows, tile) * div_up(n, tile);
+    AP_REQUIRE(tiles < (1ll << 31) / 512, "rows x n is too large");
+    p.group = (int32_t)std::min<int64_t>(div_up(rows, tile), 8);
+    const dim3 grid((unsigned)tiles);
+    if (tile == 256) hipLaunchKernelGGL((k_scores8<256, 256, 2, 4>), grid, dim3(512), 0, st, p);
+    else if (tile == 128) hipLaunchKernelGGL((k_scores8<128, 128, 2, 2>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_scores8<64, 64, 2, 2>), grid, dim3(256), 0, st, p);
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}

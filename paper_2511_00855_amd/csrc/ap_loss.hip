@@ -1,0 +1,712 @@
+// The softmax loss of queries over all documents, and its gradients.
+//
+//   l_qj = scale <x_q, w_j>,   lse_q = ln sum_j exp(l_qj),   loss_q = lse_q - l_q,label(q)
+//   c_qj = g_q (exp(l_qj - lse_q) - [j = label(q)]),   dX = scale C W,   dW = scale C^T X
+//
+// The logits are never in memory.  A tile of 256 documents x 256 queries leaves a maximum and a sum of every query behind
+// (documents are the product's rows: a lane then holds one query and 64 documents of it, and reduces them in registers);
+// the gradients make the coefficients C again, a piece of the documents at a time, in 16 bits, and multiply them out of
+// there.  bf16 rows are multiplied as they are.  f32 rows are each the sum of two f16 numbers (after one power of two for
+// the whole array, so that its largest value lies below 2^15: 22 bits of every value within 2^17 of the largest, and the
+// same absolute error below), and so are the coefficients: three products on the f16 instruction instead of one on the f32
+// instruction, which is 16 times slower.
+#include <math.h>
+#include <stdlib.h>
+#include <algorithm>
+#include <type_traits>
+#include "ap_gemm.hpp"
+#include "ap_stream.hpp"
+
+#define AP_LOG2E 1.44269504088896340736f
+#define AP_LOG2E_LO 1.92596299112661746887e-8f   // log2(e) - AP_LOG2E
+#define AP_LN2 0.69314718055994530942f
+#define AP_COEF_UP 14                            // f16 coefficients are stored times 2^14: they are at most 1
+
+// ------------------------------------------------------------------ f32 rows as two f16 parts
+// Largest finite magnitude of two arrays of rows, as the bits of a float (which are in the order of the numbers).
+struct ApSide { const float *p; int64_t ld, rows; };
+__global__ __launch_bounds__(256) void k_loss_amax(ApSide a, ApSide b, int32_t dim, uint32_t *__restrict__ out /* [2], zero */) {
+    const int32_t per = dim / 4;
+    for (int side = 0; side < 2; side++) {
+        const ApSide s = side ? b : a;
+        float m = 0.f;
+        for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < s.rows; r += (int64_t)gridDim.x * 4)
+            for (int32_t c = threadIdx.x & 63; c < per; c += 64) {
+                const float4 v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c * 4);
+                const float x[4] = {fabsf(v.x), fabsf(v.y), fabsf(v.z), fabsf(v.w)};
+#pragma unroll
+                for (int i = 0; i < 4; i++) m = x[i] > m && x[i] < INFINITY ? x[i] : m;
+            }
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        if ((threadIdx.x & 63) == 0 && m > 0.f) atomicMax(&out[side], __float_as_uint(m));
+    }
+}
+// The power of two that brings a largest magnitude into [2^14, 2^15).
+__device__ __forceinline__ int ap_loss_up(uint32_t amax) { return amax ? 14 - ilogbf(__uint_as_float(amax)) : 0; }
+
+// Rows in two f16 parts, `pad` columns each (zeros after the last).  Rows that `coef` gives 0 become zeros.
+__global__ __launch_bounds__(256) void k_loss_split(ApSide s, int32_t dim, int32_t pad, const uint32_t *__restrict__ amax, const float *__restrict__ coef,
+                                                    _Float16 *__restrict__ hi, _Float16 *__restrict__ lo) {
+    const int up = ap_loss_up(*amax);
+    const int32_t per = pad / 4;
+    for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < s.rows; r += (int64_t)gridDim.x * 4) {
+        const bool used = !coef || coef[r] != 0.f;
+        for (int32_t c = threadIdx.x & 63; c < per; c += 64) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (used && c * 4 < dim) v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c * 4);
+            const float x[4] = {v.x, v.y, v.z, v.w};
+            _Float16 h[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const float y = ldexpf(x[i], up);
+                h[i] = (_Float16)y;
+                l[i] = (_Float16)(y - (float)h[i]);
+            }
+            *reinterpret_cast<uint2 *>(hi + r * pad + c * 4) = *reinterpret_cast<const uint2 *>(h);
+            *reinterpret_cast<uint2 *>(lo + r * pad + c * 4) = *reinterpret_cast<const uint2 *>(l);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the logits' tiles
+struct ApLoss {
+    const char *docs, *x;          // 16-bit rows: as given, or their first parts
+    int64_t ldd, ldx;              // bytes from row to row
+    int64_t d_part, x_part;        // bytes from the first parts to the second
+    const uint32_t *amax;          // of the documents and the queries (two parts)
+    int64_t first;                 // first document of the piece
+    int32_t count, rows, dim;      // documents of the piece, queries, columns
+    float scale;
+    const int32_t *labels;
+    int32_t group;                 // column tiles that an XCD's workgroups take together
+    float2 *part;                  // loss: [row tile][query] maximum, sum
+    float *at_label;               // loss: the label's product
+    const float *lse, *coef;       // gradient: of each query; g_q over the largest, 0 where it has no label
+    char *c;                       // gradient: coefficients [query][document of the piece]
+    int64_t ldc, c_part;           // in bytes; c_part 0: coefficients of one part
+};
+
+// What a product becomes a logit times log2(e) by: two factors, each of which is a number where their product may not be.  Maxima and the label's
+// product are kept as they are and only differences are multiplied (the factors are positive): a loss much smaller than its logits keeps
+// its bits.
+struct ApFactor {
+    float a, b;
+    __device__ __forceinline__ ApFactor(float scale, const uint32_t *amax) : a(scale * AP_LOG2E), b(1.f) {
+        if (amax) { a = ldexpf(a, -ap_loss_up(amax[0])); b = ldexpf(b, -ap_loss_up(amax[1])); }
+    }
+    template <bool PARTS> __device__ __forceinline__ float of(float v) const { return PARTS ? v * a * b : v * a; }
+};
+
+__device__ __forceinline__ uint32_t ap_bf16_pair(float a, float b) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// Two (maximum, sum) pairs become one.
+template <bool PARTS> __device__ __forceinline__ void ap_lse_join(float &m, float &s, float m2, float s2, const ApFactor &f) {
+    const float t = fmaxf(m, m2), base = t == -INFINITY ? 0.f : t;
+    s = s * __builtin_amdgcn_exp2f(f.of<PARTS>(m - base)) + s2 * __builtin_amdgcn_exp2f(f.of<PARTS>(m2 - base));
+    m = t;
+}
+
+// Coefficients of four documents in a row of one query: v are the logits times log2(e), g its weight (0: none), `at` where its label lies from
+// the first on, `docs` how many of them there are.
+struct ApCoef {
+    float g, lse2, lse2_lo;
+    __device__ __forceinline__ ApCoef(float g_, float lse) : g(g_), lse2(lse * AP_LOG2E) { lse2_lo = fmaf(lse, AP_LOG2E, -lse2) + lse * AP_LOG2E_LO; }
+    template <bool PARTS> __device__ __forceinline__ void put(const float *v, int64_t at, int64_t docs, char *to, int64_t c_part) const {
+        float c[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float e = __builtin_amdgcn_exp2f((v[i] - lse2) - lse2_lo);
+            if (at == i) e -= 1.f;
+            c[i] = g != 0.f && i < docs ? e * g : 0.f;
+        }
+        if (PARTS) {
+            _Float16 h[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const float y = ldexpf(c[i], AP_COEF_UP);
+                h[i] = (_Float16)y;
+                l[i] = (_Float16)(y - (float)h[i]);
+            }
+            *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(h);
+            *reinterpret_cast<uint2 *>(to + c_part) = *reinterpret_cast<const uint2 *>(l);
+        } else {
+            const uint2 h = make_uint2(ap_bf16_pair(c[0], c[1]), ap_bf16_pair(c[2], c[3]));
+            *reinterpret_cast<uint2 *>(to) = h;
+            if (c_part)
+                *reinterpret_cast<uint2 *>(to + c_part) = make_uint2(ap_bf16_pair(c[0] - __uint_as_float(h.x << 16), c[1] - __uint_as_float(h.x & 0xffff0000u)),
+                                                                     ap_bf16_pair(c[2] - __uint_as_float(h.y << 16), c[3] - __uint_as_float(h.y & 0xffff0000u)));
+        }
+    }
+};
+
+// GRAD: the tile's coefficients.  Otherwise its maximum and sum a query.
+template <class OP, int TM, int TN, int WM, int WN, bool PARTS, bool GRAD>
+__global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
+    using G = ApGemm<OP, TM, TN, WM, WN, true, true>;
+    __shared__ __attribute__((aligned(1024))) char lds[G::LDS_BYTES];
+    uint32_t mt, nt;
+    ap_g_tile(blockIdx.x, (p.count + TM - 1) / TM, (p.rows + TN - 1) / TN, p.group, &mt, &nt);
+    const int32_t m0 = mt * TM, n0 = nt * TN;
+    const int32_t docs = min(TM, p.count - m0), queries = min(TN, p.rows - n0);
+    typename G::Acc acc[G::FA][G::FB];
+    G::product({p.docs + (p.first + m0) * p.ldd, p.ldd, docs}, {p.x + n0 * p.ldx, p.ldx, queries}, p.dim, PARTS ? 3 : 1, p.d_part, p.x_part, lds, acc);
+
+    const int lane = threadIdx.x & 63, wave = ap_wave_id(), wm = wave / WN, wn = wave % WN;
+    const ApFactor f(p.scale, PARTS ? p.amax : nullptr);
+    const int row0 = wm * (TM / WM) + 4 * (lane >> 5);   // of block a, register r: row0 + 32 a + 8 (r / 4) + r % 4
+    float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + WM * TN;
+#pragma unroll
+    for (int b = 0; b < G::FB; b++) {
+        const int col = wn * (TN / WN) + b * 32 + (lane & 31);
+        const bool is = col < queries;
+        const int32_t label = is ? p.labels[n0 + col] : -1;
+        const int64_t local = (int64_t)label - p.first - m0 - row0;   // of the label among this lane's rows
+        if (!GRAD) {
+            if (label >= 0 && local >= 0 && local < TM / WM && !(local & 4)) {
+#pragma unroll
+                for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        if (local == a * 32 + 8 * (r >> 2) + (r & 3) && local + row0 < docs) p.at_label[n0 + col] = acc[a][b][r];
+            }
+            if (docs < TM)
+#pragma unroll
+                for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        if (row0 + a * 32 + 8 * (r >> 2) + (r & 3) >= docs) acc[a][b][r] = -INFINITY;
+            float m = -INFINITY;
+#pragma unroll
+            for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) m = fmaxf(m, acc[a][b][r]);
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            const float base = m == -INFINITY ? 0.f : m;
+            float s = 0.f;
+#pragma unroll
+            for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) s += __builtin_amdgcn_exp2f(f.of<PARTS>(acc[a][b][r] - base));
+            s += __shfl_xor(s, 32, 64);
+            if (lane < 32) { s_max[wm * TN + col] = m; s_sum[wm * TN + col] = s; }
+        } else {
+            const ApCoef coef(is ? p.coef[n0 + col] : 0.f, is ? p.lse[n0 + col] : 0.f);
+            char *to = p.c + (int64_t)(n0 + col) * p.ldc + (m0 + row0) * 2;
+#pragma unroll
+            for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int at = a * 32 + 2 * r;
+                    const float v[4] = {f.of<PARTS>(acc[a][b][r]), f.of<PARTS>(acc[a][b][r + 1]), f.of<PARTS>(acc[a][b][r + 2]), f.of<PARTS>(acc[a][b][r + 3])};
+                    if (is) coef.put<PARTS>(v, local - at, docs - row0 - at, to + at * 2, p.c_part);
+                }
+        }
+    }
+    if (!GRAD) {
+        __syncthreads();
+        for (int col = threadIdx.x; col < queries; col += WM * WN * 64) {
+            float m = s_max[col], s = s_sum[col];
+            for (int w = 1; w < WM; w++) ap_lse_join<PARTS>(m, s, s_max[w * TN + col], s_sum[w * TN + col], f);
+            p.part[(int64_t)mt * p.rows + n0 + col] = make_float2(m, s);
+        }
+    }
+}
+
+// Joins the (maximum, sum) pairs of a query.  1,024 threads take 2^qb queries; the pairs of a query are shared out to 1024 / 2^qb threads
+// and joined in a fixed tree.
+__global__ __launch_bounds__(1024) void k_loss_join(const float2 *__restrict__ part, int64_t tiles, int32_t rows, int qb, const int32_t *__restrict__ labels, int32_t n,
+                                                    const float *__restrict__ at_label, float scale, const uint32_t *__restrict__ amax, float *__restrict__ loss, float *__restrict__ lse) {
+    const ApFactor f(scale, amax);
+    __shared__ float s_m[1024], s_s[1024];
+    const int32_t q = (blockIdx.x << qb) + (threadIdx.x & ((1 << qb) - 1));
+    float m = -INFINITY, s = 0.f;
+    if (q < rows)
+        for (int64_t t = threadIdx.x >> qb; t < tiles; t += 1024 >> qb) {
+            const float2 v = part[t * rows + q];
+            ap_lse_join<true>(m, s, v.x, v.y, f);
+        }
+    s_m[threadIdx.x] = m;
+    s_s[threadIdx.x] = s;
+    for (int o = 512; o >= 1 << qb; o >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < o) {
+            ap_lse_join<true>(m, s, s_m[threadIdx.x + o], s_s[threadIdx.x + o], f);
+            s_m[threadIdx.x] = m;
+            s_s[threadIdx.x] = s;
+        }
+    }
+    if ((int)threadIdx.x < 1 << qb && q < rows) {
+        const float sum = log2f(s);
+        lse[q] = (f.of<true>(m) + sum) * AP_LN2;
+        const int32_t label = labels[q];
+        loss[q] = label >= 0 && label < n ? (f.of<true>(m - at_label[q]) + sum) * AP_LN2 : 0.f;
+    }
+}
+
+// Few queries: one pass over the documents as they are (f32 rows by the f32 instruction: memory is slower).  A lane has one query and four
+// documents at a time; a workgroup leaves one pair of every query behind.
+template <int DT, int NQ, bool GRAD>
+__global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int SIZE = DT == AP_F32 ? 4 : 2;
+    const int lane = threadIdx.x & 63, wave = ap_wave_id(), bytes = p.dim * SIZE, groups = (bytes + 63) / 64 * 4;
+    for (int i = threadIdx.x; i < NQ * 16 * groups; i += AP_STREAM_THREADS) {
+        const int q = i / groups, c = i % groups * 16;
+        *reinterpret_cast<uint4 *>(lds + ap_stream_place(q, c, NQ)) = q < p.rows && c < bytes ? *reinterpret_cast<const uint4 *>(p.x + q * p.ldx + c) : make_uint4(0, 0, 0, 0);
+    }
+    float m[NQ], s[NQ];
+    int32_t label[NQ];
+#pragma unroll
+    for (int g = 0; g < NQ; g++) {
+        const int q = g * 16 + (lane & 15);
+        m[g] = -INFINITY;
+        s[g] = 0.f;
+        label[g] = q < p.rows ? p.labels[q] : -1;
+    }
+    __syncthreads();
+    const ApFactor f(p.scale, nullptr);
+    using OP = typename std::conditional<DT == AP_F32, ApStreamF32, ApStreamBf16>::type;
+    const int64_t wave0 = (int64_t)blockIdx.x * (AP_STREAM_THREADS / 64) + wave, waves = (int64_t)gridDim.x * (AP_STREAM_THREADS / 64);
+    if constexpr (GRAD) {   // the same products as the loss took, bit for bit: what is off in a logit is off in lse too
+        float coef[NQ], lse[NQ];
+#pragma unroll
+        for (int g = 0; g < NQ; g++) {
+            const int q = g * 16 + (lane & 15);
+            coef[g] = q < p.rows ? p.coef[q] : 0.f;
+            lse[g] = q < p.rows ? p.lse[q] : 0.f;
+        }
+        ap_stream<OP, NQ>(p.docs + p.first * p.ldd, p.ldd, p.count, bytes, lds, wave0, waves, [&](int64_t first, const ap_s_f32x4 (&acc)[NQ]) {
+            const int64_t d = first + (lane >> 4) * 4;
+#pragma unroll
+            for (int g = 0; g < NQ; g++) {
+                const int q = g * 16 + (lane & 15);
+                if (q >= p.rows) continue;
+                const float v[4] = {f.of<false>(acc[g][0]), f.of<false>(acc[g][1]), f.of<false>(acc[g][2]), f.of<false>(acc[g][3])};
+                ApCoef(coef[g], lse[g]).put<DT == AP_F32>(v, label[g] - p.first - d, p.count - d, p.c + q * p.ldc + d * 2, p.c_part);
+            }
+        });
+        return;
+    }
+    ap_stream<OP, NQ>(p.docs, p.ldd, p.count, bytes, lds, wave0, waves,
+                      [&](int64_t first, const ap_s_f32x4 (&acc)[NQ]) {
+                          const int64_t d = first + (lane >> 4) * 4;
+#pragma unroll
+                          for (int g = 0; g < NQ; g++) {
+                              float v[4], t = m[g];
+#pragma unroll
+                              for (int r = 0; r < 4; r++) {
+                                  v[r] = d + r < p.count ? acc[g][r] : -INFINITY;
+                                  if (label[g] >= 0 && label[g] == d + r && d + r < p.count) p.at_label[g * 16 + (lane & 15)] = v[r];
+                                  t = fmaxf(t, v[r]);
+                              }
+                              const float base = t == -INFINITY ? 0.f : t;
+                              s[g] *= __builtin_amdgcn_exp2f(f.of<false>(m[g] - base));
+#pragma unroll
+                              for (int r = 0; r < 4; r++) s[g] += __builtin_amdgcn_exp2f(f.of<false>(v[r] - base));
+                              m[g] = t;
+                          }
+                      });
+    __syncthreads();   // the queries are not needed any more
+    float (*s_m)[NQ * 16] = reinterpret_cast<float (*)[NQ * 16]>(lds), (*s_s)[NQ * 16] = s_m + AP_STREAM_THREADS / 64;
+#pragma unroll
+    for (int g = 0; g < NQ; g++) {
+        ap_lse_join<false>(m[g], s[g], __shfl_xor(m[g], 16, 64), __shfl_xor(s[g], 16, 64), f);
+        ap_lse_join<false>(m[g], s[g], __shfl_xor(m[g], 32, 64), __shfl_xor(s[g], 32, 64), f);
+        if (lane < 16) { s_m[wave][g * 16 + lane] = m[g]; s_s[wave][g * 16 + lane] = s[g]; }
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < p.rows; q += AP_STREAM_THREADS) {
+        float a = s_m[0][q], b = s_s[0][q];
+        for (int w = 1; w < AP_STREAM_THREADS / 64; w++) ap_lse_join<false>(a, b, s_m[w][q], s_s[w][q], f);
+        p.part[(int64_t)blockIdx.x * p.rows + q] = make_float2(a, b);
+    }
+}
+
+// ------------------------------------------------------------------ the gradients' products
+// *most = the largest |g_q| of the queries that have a label (1 if there is none): the coefficients are stored relative to it, so
+// that equal weights leave the label's own coefficient p - 1 without a rounding of the weight.
+__global__ __launch_bounds__(1024) void k_loss_most(const float *__restrict__ g, const int32_t *__restrict__ labels, int32_t rows, int32_t n, float *__restrict__ most,
+                                                    float *__restrict__ coef) {
+    __shared__ float s_m[16];
+    float m = 0.f;
+    for (int32_t q = threadIdx.x; q < rows; q += 1024)
+        if (labels[q] >= 0 && labels[q] < n) { const float v = fabsf(g[q]); m = v > m && v < INFINITY ? v : m; }
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = 0.f;
+    for (int w = 0; w < 16; w++) m = fmaxf(m, s_m[w]);
+    if (m == 0.f) m = 1.f;
+    if (threadIdx.x == 0) *most = m;
+    for (int32_t q = threadIdx.x; q < rows; q += 1024) coef[q] = labels[q] >= 0 && labels[q] < n ? g[q] / m : 0.f;
+}
+
+// bf16 queries without those that have no weight: what is multiplied by 0 must not be infinite or NaN
+__global__ __launch_bounds__(256) void k_loss_used(const char *__restrict__ x, int64_t ld, int32_t rows, int32_t groups, const float *__restrict__ coef, uint4 *__restrict__ out) {
+    const int64_t total = (int64_t)rows * groups;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / groups, c = i % groups;
+        out[i] = coef[r] != 0.f ? *reinterpret_cast<const uint4 *>(x + r * ld + c * 16) : make_uint4(0, 0, 0, 0);
+    }
+}
+
+struct ApLossGrad {
+    const char *c;                 // coefficients [query][document of the piece]
+    int64_t ldc, c_part;
+    const char *docs, *x;
+    int64_t ldd, ldx, d_part, x_part;
+    const uint32_t *amax;
+    int64_t first;
+    int32_t count, rows, dim;
+    float scale;
+    const float *most;
+    void *grad_docs;               // NULL: not wanted
+    int64_t ld_out;
+    float *gx;                     // NULL: not wanted; [split][query][dim], sums so far
+    int32_t splits, split_docs;    // the documents of the piece in `splits` runs of `split_docs`
+    int32_t tiles_docs;            // workgroups of the documents' gradient; the others make the queries'
+    int32_t parts;                 // pairs of parts that are multiplied: 1, 2 (two parts of the coefficients), 3 (of both factors)
+    int32_t start;                 // 1: first piece, nothing is there to add to
+};
+
+template <class OP, int TM, int TN, int WM, int WN, bool PARTS>
+__global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
+    using GD = ApGemm<OP, TM, TN, WM, WN, false, false>;
+    using GX = ApGemm<OP, TM, TN, WM, WN, true, false>;
+    __shared__ __attribute__((aligned(1024))) char lds[GD::LDS_BYTES];
+    const uint32_t nt = (p.dim + TN - 1) / TN;
+    typename GD::Acc acc[GD::FA][GD::FB];
+    if ((int32_t)blockIdx.x < p.tiles_docs) {
+        uint32_t m, n;
+        ap_g_tile(blockIdx.x, (p.count + TM - 1) / TM, nt, nt, &m, &n);
+        const int32_t m0 = m * TM, n0 = n * TN, docs = min(TM, p.count - m0), cols = min(TN, p.dim - n0);
+        GD::product({p.c + m0 * 2, p.ldc, docs * 2}, {p.x + n0 * 2, p.ldx, cols * 2}, p.rows, p.parts, p.c_part, p.x_part, lds, acc);
+        float f1 = p.scale, f2 = *p.most;
+        if (PARTS) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(p.amax[1])); }
+        const int64_t at0 = (p.first + m0) * p.ld_out + n0;
+        GD::each(acc, [&](int i, int j, float v) {
+            if (i >= docs || j >= cols) return;
+            v = v * f1 * f2;
+            if (PARTS) static_cast<float *>(p.grad_docs)[at0 + i * p.ld_out + j] = v;
+            else static_cast<__bf16 *>(p.grad_docs)[at0 + i * p.ld_out + j] = (__bf16)v;
+        });
+        return;
+    }
+    const uint32_t mt = (p.rows + TM - 1) / TM, block = blockIdx.x - p.tiles_docs;
+    const uint32_t split = block / (mt * nt), t = block % (mt * nt), m0 = t / nt * TM, n0 = t % nt * TN;
+    const int32_t queries = min(TM, p.rows - (int32_t)m0), cols = min(TN, p.dim - (int32_t)n0);
+    const int64_t d0 = (int64_t)split * p.split_docs, docs = min((int64_t)p.split_docs, p.count - d0);
+    GX::product({p.c + m0 * p.ldc + d0 * 2, p.ldc, queries}, {p.docs + (p.first + d0) * p.ldd + n0 * 2, p.ldd, cols * 2}, docs > 0 ? docs : 0, p.parts, p.c_part, p.d_part, lds, acc);
+    float *to = p.gx + ((int64_t)split * p.rows + m0) * p.dim + n0;
+    GX::each(acc, [&](int i, int j, float v) {
+        if (i >= queries || j >= cols) return;
+        float *at = to + (int64_t)i * p.dim + j;
+        *at = p.start ? v : *at + v;
+    });
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, int32_t splits, int32_t rows, int32_t dim, float scale, const float *__restrict__ most,
+                                                 const uint32_t *__restrict__ amax, void *__restrict__ out, int64_t ld) {
+    const int64_t total = (int64_t)rows * dim / 4;
+    float f1 = scale, f2 = *most;
+    if (!BF16) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(amax[0])); }
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int32_t k = 0; k < splits; k++) {
+            const float4 v = reinterpret_cast<const float4 *>(gx)[k * total + i];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        s.x = s.x * f1 * f2; s.y = s.y * f1 * f2; s.z = s.z * f1 * f2; s.w = s.w * f1 * f2;
+        const int64_t r = i / (dim / 4), c = i % (dim / 4) * 4;
+        if (BF16) *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + r * ld + c) = make_uint2(ap_bf16_pair(s.x, s.y), ap_bf16_pair(s.z, s.w));
+        else *reinterpret_cast<float4 *>(static_cast<float *>(out) + r * ld + c) = s;
+    }
+}
+
+// ------------------------------------------------------------------ host side
+static int64_t up_to(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+static int64_t div_up(int64_t v, int64_t m) { return (v + m - 1) / m; }
+
+// The workspace of one call: arrays one after the other, each at a multiple of 256 bytes.  Without a base it is only measured.
+struct LossWs {
+    char *base;
+    size_t bytes = 0;
+    template <class T> T *take(int64_t count) {
+        T *p = base ? reinterpret_cast<T *>(base + bytes) : nullptr;
+        bytes += up_to(count * (int64_t)sizeof(T), 256);
+        return p;
+    }
+};
+
+static int check_rows(const char *what, const void *p, int64_t ld, int32_t dim, int32_t dtype) {
+    AP_REQUIRE(p != nullptr, "%s is NULL", what);
+    AP_REQUIRE(((uintptr_t)p & 15) == 0, "%s must be 16-byte aligned", what);
+    const int group = dtype == AP_BF16 ? 8 : 4;
+    AP_REQUIRE(ld >= dim && ld % group == 0 && ld <= (1 << 20), "%s: %lld elements from row to row, must be a multiple of %d in [dim, 2^20]", what, (long long)ld, group);
+    return AP_OK;
+}
+static int check_scale(float scale) {
+    AP_REQUIRE(scale > 0.f && scale < INFINITY, "scale = %g must be a positive number", scale);
+    return AP_OK;
+}
+static int check_sizes(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
+    AP_REQUIRE(dtype == AP_F32 || dtype == AP_BF16, "dtype = %d is not AP_F32/AP_BF16", dtype);
+    const int group = dtype == AP_BF16 ? 8 : 4;
+    AP_REQUIRE(dim >= group && dim % group == 0 && dim <= 8192, "dim = %d must be a multiple of %d and at most 8192", dim, group);
+    AP_REQUIRE(rows >= 0 && rows <= (1 << 24), "rows = %lld must be in [0, 2^24]", (long long)rows);
+    AP_REQUIRE(n >= 1 && n < (1ll << 30), "n = %lld must be in [1, 2^30)", (long long)n);
+    return AP_OK;
+}
+
+struct LossParts {   // f32 rows as two f16 parts
+    uint32_t *amax = nullptr;
+    _Float16 *docs = nullptr, *x = nullptr;
+    int64_t pad = 0, d_part = 0, x_part = 0;
+    void take(LossWs &ws, int64_t rows, int64_t n, int32_t dim) {
+        pad = up_to(dim, 8);
+        amax = ws.take<uint32_t>(2);
+        docs = ws.take<_Float16>(2 * n * pad);
+        x = ws.take<_Float16>(2 * rows * pad);
+        d_part = n * pad * 2;
+        x_part = rows * pad * 2;
+    }
+    int make(const void *xp, int64_t ldx, int64_t rows, const void *dp, int64_t ldd, int64_t n, int32_t dim, const float *coef, hipStream_t st) {
+        const ApSide sd = {static_cast<const float *>(dp), ldd, n}, sx = {static_cast<const float *>(xp), ldx, rows};
+        AP_TRY(ap_fill_u32(amax, 2, 0, st));
+        hipLaunchKernelGGL(k_loss_amax, dim3((unsigned)std::min<int64_t>(div_up(n, 4), 2048)), dim3(256), 0, st, sd, sx, dim, amax);
+        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(n, 4), 4096)), dim3(256), 0, st, sd, dim, (int32_t)pad, amax, nullptr, docs, docs + n * pad);
+        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(rows, 4), 4096)), dim3(256), 0, st, sx, dim, (int32_t)pad, amax + 1, coef, x, x + rows * pad);
+        AP_CHECK_HIP(hipGetLastError());
+        return AP_OK;
+    }
+};
+
+// The tile that fills the compute units: the largest of 256, 128, 64 whose tiles are at least 3/4 of them.
+static int pick_tile(int64_t m, int64_t n) {
+    for (int t = 256; t > 64; t /= 2)
+        if (div_up(m, t) * div_up(n, t) >= 192) return t;
+    return 64;
+}
+
+template <class OP, bool PARTS, bool GRAD>
+static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
+    const int64_t mt = div_up(p.count, tile), nt = div_up(p.rows, tile);
+    AP_REQUIRE(mt * nt < (1ll << 31) / 512, "rows x n is too large");
+    const dim3 grid((unsigned)(mt * nt));
+    p.group = (int32_t)std::min<int64_t>(nt, 8);
+    if (tile == 256) hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
+    else if (tile == 128) hipLaunchKernelGGL((k_loss_tiles<OP, 128, 128, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_loss_tiles<OP, 64, 64, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}
+
+// Up to how many queries one pass over the documents pays.
+static bool loss_few(int64_t rows, int32_t dim, int32_t dtype) { return rows <= 64 && ap_stream_lds(rows, (int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) <= AP_STREAM_LDS; }
+
+static int64_t few_blocks(int64_t n) { return std::min<int64_t>(div_up(n, 16 * AP_STREAM_THREADS / 64), 512); }
+
+template <int DT, bool GRAD> static int launch_few(const ApLoss &p, hipStream_t st) {
+    // the pairs of the waves take the queries' place
+    const size_t lds = (size_t)std::max<int64_t>(ap_stream_lds(p.rows, (int64_t)p.dim * (DT == AP_F32 ? 4 : 2)), div_up(p.rows, 16) * 16 * 8 * (AP_STREAM_THREADS / 64));
+    const int64_t blocks = few_blocks(p.count);
+    const dim3 grid((unsigned)blocks);
+#define AP_FEW(N)                                                                                                                       \
+    case N:                                                                                                                             \
+        if (lds > 60 * 1024) AP_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_loss_few<DT, N, GRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
+        hipLaunchKernelGGL((k_loss_few<DT, N, GRAD>), grid, dim3(AP_STREAM_THREADS), lds, st, p);                                             \
+        break
+    switch ((p.rows + 15) / 16) { AP_FEW(1); AP_FEW(2); AP_FEW(3); AP_FEW(4); }
+#undef AP_FEW
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}
+
+struct LossPlan {
+    int tile;
+    bool few;
+    int64_t pairs;                 // of every query
+    float2 *part;
+    float *at_label;
+    LossParts parts;
+    size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
+        LossWs ws{base};
+        few = loss_few(rows, dim, dtype);
+        tile = pick_tile(n, rows);
+        pairs = few ? few_blocks(n) : div_up(n, tile);
+        part = ws.take<float2>(pairs * rows);
+        at_label = ws.take<float>(rows);
+        if (dtype == AP_F32 && !few) parts.take(ws, rows, n, dim);
+        return ws.bytes;
+    }
+};
+
+extern "C" int ap_softmax_loss_bytes(int64_t rows, int64_t n, int32_t dim, int32_t dtype, size_t *out) {
+    AP_REQUIRE(out != nullptr, "out is NULL");
+    AP_TRY(check_sizes(rows, n, dim, dtype));
+    LossPlan plan;
+    *out = plan.lay(nullptr, rows, n, dim, dtype);
+    return AP_OK;
+}
+
+extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const void *docs, int64_t ldd, int64_t n, int32_t dim, int32_t dtype, float scale,
+                               const int32_t *labels, float *loss, float *lse, void *workspace, size_t bytes, void *stream) {
+    AP_TRY(check_sizes(rows, n, dim, dtype));
+    AP_TRY(check_scale(scale));
+    if (rows == 0) return AP_OK;
+    AP_TRY(check_rows("x", x, ldx, dim, dtype));
+    AP_TRY(check_rows("docs", docs, ldd, dim, dtype));
+    AP_REQUIRE(labels && loss && lse, "labels, loss or lse is NULL");
+    LossPlan plan;
+    const size_t need = plan.lay(static_cast<char *>(workspace), rows, n, dim, dtype);
+    AP_REQUIRE(workspace && bytes >= need, "workspace of %zu bytes, %zu are needed", bytes, need);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    ApLoss p{};
+    p.count = (int32_t)n; p.rows = (int32_t)rows; p.scale = scale; p.labels = labels; p.part = plan.part; p.at_label = plan.at_label;
+    if (plan.few) {
+        const int64_t size = dtype == AP_BF16 ? 2 : 4;
+        p.docs = static_cast<const char *>(docs); p.x = static_cast<const char *>(x); p.ldd = ldd * size; p.ldx = ldx * size; p.dim = dim;
+        AP_TRY((dtype == AP_BF16 ? launch_few<AP_BF16, false>(p, st) : launch_few<AP_F32, false>(p, st)));
+    } else if (dtype == AP_F32) {
+        AP_TRY(plan.parts.make(x, ldx, rows, docs, ldd, n, dim, nullptr, st));
+        p.docs = (const char *)plan.parts.docs; p.x = (const char *)plan.parts.x; p.ldd = p.ldx = plan.parts.pad * 2;
+        p.d_part = plan.parts.d_part; p.x_part = plan.parts.x_part; p.amax = plan.parts.amax; p.dim = (int32_t)plan.parts.pad;
+        AP_TRY((launch_tiles<ApF16Op, true, false>(p, plan.tile, st)));
+    } else {
+        p.docs = static_cast<const char *>(docs); p.x = static_cast<const char *>(x); p.ldd = ldd * 2; p.ldx = ldx * 2; p.dim = dim;
+        AP_TRY((launch_tiles<ApBf16Op, false, false>(p, plan.tile, st)));
+    }
+    int qb = 0;
+    while (qb < 6 && (1 << qb) < rows) qb++;
+    hipLaunchKernelGGL(k_loss_join, dim3((unsigned)div_up(rows, 1 << qb)), dim3(1024), 0, st, plan.part, plan.pairs, (int32_t)rows, qb, labels, (int32_t)n,
+                       plan.at_label, scale, p.amax, loss, lse);
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}
+
+#define AP_LOSS_PIECE_BYTES ((int64_t)128 << 20)   // of the coefficients of a piece, one part: they stay in the last cache until they are multiplied
+
+struct GradPlan {
+    int64_t piece, ldc, c_part;
+    int tile_c, tile;
+    bool few, two;
+    int32_t splits, split_docs;
+    float *most, *coef, *gx;
+    char *c, *x;
+    LossParts parts;
+    size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype, bool want_x) {
+        LossWs ws{base};
+        const int64_t r = std::max<int64_t>(rows, 1);
+        piece = std::max<int64_t>(AP_LOSS_PIECE_BYTES / (2 * r) / 256 * 256, 1024);
+        if (g_ap_debug.loss_piece) piece = up_to(g_ap_debug.loss_piece, 256);
+        piece = std::min(piece, up_to(n, 256));
+        ldc = piece * 2;
+        // bf16 coefficients of few queries have a second part: a rounding of the label's alone would be seen in the result, and
+        // where few are multiplied at once the second product costs little
+        two = dtype == AP_BF16 && r <= 128;
+        c_part = r * ldc;
+        few = loss_few(r, dim, dtype);
+        tile_c = pick_tile(piece, r);
+        tile = pick_tile(piece, dim);
+        if (tile > 128 && r <= 128) tile = 128;
+        if (tile > 64 && r <= 64) tile = 64;
+        // the queries' gradient: as much work a workgroup as the documents' has, and no fewer workgroups than fill the compute units
+        const int64_t tiles = div_up(r, tile) * div_up(dim, tile);
+        const int64_t by_work = div_up(piece, std::max<int64_t>(r, 512)), by_cus = div_up(256, tiles);
+        splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({std::max(by_work, by_cus), div_up(piece, 256), 64}));
+        split_docs = (int32_t)up_to(div_up(piece, splits), 64);
+        splits = (int32_t)div_up(piece, split_docs);
+        most = ws.take<float>(1);
+        coef = ws.take<float>(r);
+        c = ws.take<char>(c_part * (dtype == AP_F32 || two ? 2 : 1));
+        gx = want_x ? ws.take<float>(splits * r * dim) : nullptr;
+        if (dtype == AP_F32) parts.take(ws, r, n, dim);
+        else x = ws.take<char>(r * dim * 2);
+        return ws.bytes;
+    }
+};
+
+extern "C" int ap_softmax_loss_grad_bytes(int64_t rows, int64_t n, int32_t dim, int32_t dtype, int32_t want_x, size_t *out) {
+    AP_REQUIRE(out != nullptr, "out is NULL");
+    AP_TRY(check_sizes(rows, n, dim, dtype));
+    GradPlan plan;
+    *out = plan.lay(nullptr, rows, n, dim, dtype, want_x != 0);
+    return AP_OK;
+}
+
+template <class OP, bool PARTS>
+static int loss_pieces(const GradPlan &plan, ApLoss p, const ApLoss &few, ApLossGrad g, int64_t n, hipStream_t st) {
+    for (int64_t d0 = 0; d0 < n; d0 += plan.piece) {
+        p.first = g.first = d0;
+        p.count = g.count = (int32_t)std::min(plan.piece, n - d0);
+        if (plan.few) {
+            ApLoss f = p;
+            f.docs = few.docs; f.x = few.x; f.ldd = few.ldd; f.ldx = few.ldx; f.dim = few.dim;
+            AP_TRY((launch_few<PARTS ? AP_F32 : AP_BF16, true>(f, st)));
+        } else {
+            AP_TRY((launch_tiles<OP, PARTS, true>(p, plan.tile_c, st)));
+        }
+        const int64_t nt = div_up(g.dim, plan.tile);
+        g.tiles_docs = g.grad_docs ? (int32_t)(div_up(g.count, plan.tile) * nt) : 0;
+        g.splits = plan.splits;
+        g.split_docs = plan.split_docs;
+        g.start = d0 == 0;
+        // a short last piece leaves the runs past its end alone
+        const int64_t runs = g.start ? plan.splits : div_up(g.count, plan.split_docs);
+        const dim3 grid((unsigned)(g.tiles_docs + (g.gx ? runs * div_up(g.rows, plan.tile) * nt : 0)));
+        if (plan.tile == 256) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
+        else if (plan.tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        else hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        AP_CHECK_HIP(hipGetLastError());
+    }
+    return AP_OK;
+}
+
+extern "C" int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, const void *docs, int64_t ldd, int64_t n, int32_t dim, int32_t dtype, float scale,
+                                    const int32_t *labels, const float *lse, const float *row_grad, void *grad_x, void *grad_docs, void *workspace, size_t bytes, void *stream) {
+    AP_TRY(check_sizes(rows, n, dim, dtype));
+    AP_TRY(check_scale(scale));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rows == 0) return grad_docs ? ap_fill_u32(grad_docs, (size_t)n * dim * (dtype == AP_BF16 ? 2 : 4) / 4, 0, st) : AP_OK;
+    AP_TRY(check_rows("x", x, ldx, dim, dtype));
+    AP_TRY(check_rows("docs", docs, ldd, dim, dtype));
+    AP_REQUIRE(labels && lse && row_grad, "labels, lse or row_grad is NULL");
+    AP_REQUIRE(grad_x || grad_docs, "neither gradient is wanted");
+    AP_REQUIRE(((uintptr_t)grad_x & 15) == 0 && ((uintptr_t)grad_docs & 15) == 0, "gradients must be 16-byte aligned");
+    GradPlan plan;
+    const size_t need = plan.lay(static_cast<char *>(workspace), rows, n, dim, dtype, grad_x != nullptr);
+    AP_REQUIRE(workspace && bytes >= need, "workspace of %zu bytes, %zu are needed", bytes, need);
+    hipLaunchKernelGGL(k_loss_most, dim3(1), dim3(1024), 0, st, row_grad, labels, (int32_t)rows, (int32_t)n, plan.most, plan.coef);
+    ApLoss p{};
+    ApLossGrad g{};
+    p.rows = g.rows = (int32_t)rows;
+    p.scale = g.scale = scale;
+    p.labels = labels; p.lse = lse; p.coef = plan.coef; p.c = plan.c; p.ldc = g.ldc = plan.ldc; p.c_part = g.c_part = dtype == AP_F32 || plan.two ? plan.c_part : 0;
+    g.parts = dtype == AP_F32 ? 3 : plan.two ? 2 : 1;
+    g.c = plan.c; g.most = plan.most; g.grad_docs = grad_docs; g.ld_out = dim; g.gx = plan.gx; g.dim = dim;
+    ApLoss few = p;   // the rows as they are
+    const int64_t size = dtype == AP_BF16 ? 2 : 4;
+    few.docs = static_cast<const char *>(docs); few.x = static_cast<const char *>(x); few.ldd = ldd * size; few.ldx = ldx * size; few.dim = dim;
+    const unsigned join = (unsigned)std::min<int64_t>(div_up(rows * dim / 4, 256), 4096);
+    if (dtype == AP_F32) {
+        const LossParts &q = plan.parts;
+        AP_TRY(plan.parts.make(x, ldx, rows, docs, ldd, n, dim, plan.coef, st));
+        p.docs = g.docs = (const char *)q.docs; p.x = g.x = (const char *)q.x; p.ldd = p.ldx = g.ldd = g.ldx = q.pad * 2;
+        p.d_part = g.d_part = q.d_part; p.x_part = g.x_part = q.x_part; p.amax = g.amax = q.amax; p.dim = (int32_t)q.pad;
+        AP_TRY((loss_pieces<ApF16Op, true>(plan, p, few, g, n, st)));
+        if (grad_x) hipLaunchKernelGGL((k_loss_gx<false>), dim3(join), dim3(256), 0, st, plan.gx, plan.splits, (int32_t)rows, dim, scale, plan.most, q.amax, grad_x, (int64_t)dim);
+    } else {
+        hipLaunchKernelGGL(k_loss_used, dim3((unsigned)std::min<int64_t>(div_up(rows * dim / 8, 256), 4096)), dim3(256), 0, st, static_cast<const char *>(x), ldx * 2, (int32_t)rows,
+                           dim / 8, plan.coef, reinterpret_cast<uint4 *>(plan.x));
+        p.docs = g.docs = static_cast<const char *>(docs); p.x = g.x = plan.x; p.ldd = g.ldd = ldd * 2; p.ldx = g.ldx = (int64_t)dim * 2; p.dim = dim;
+        AP_TRY((loss_pieces<ApBf16Op, false>(plan, p, few, g, n, st)));
+        if (grad_x) hipLaunchKernelGGL((k_loss_gx<true>), dim3(join), dim3(256), 0, st, plan.gx, plan.splits, (int32_t)rows, dim, scale, plan.most, nullptr, grad_x, (int64_t)dim);
+    }
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
+}
