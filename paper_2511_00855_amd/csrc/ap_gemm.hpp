@@ -10,31 +10,32 @@
 #ifdef __HIPCC__
 typedef __bf16 ap_g_bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 ap_g_f16x8 __attribute__((ext_vector_type(8)));
-typedef float ap_g_f32x16 __attribute__((ext_vector_type(16)));
-typedef int32_t ap_g_i32x16 __attribute__((ext_vector_type(16)));
 typedef int32_t ap_g_i32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t ap_g_i32x2 __attribute__((ext_vector_type(2)));
 typedef short ap_g_s16x4 __attribute__((ext_vector_type(4)));
 
-// What is multiplied: 16 bytes of a lane, 8 values of 16 bits or 16 of 8.
+typedef float ap_g_f32x4 __attribute__((ext_vector_type(4)));
+
+// What is multiplied: 16 bytes of a lane, 8 values of 16 bits or 16 of 8, in blocks of 16 x 16.  The 32 x 32 instructions have the same rate
+// but move 8 KB of accumulators for 2 KB of operands; large products are held by the card's power, and there the 16 x 16 ones (2 KB for 2 KB)
+// are 9 % faster (8,192^3 bf16: 1.27 against 1.17 PFLOP/s).
 struct ApBf16Op {
-    typedef ap_g_f32x16 Acc;
+    typedef ap_g_f32x4 Acc;
     static constexpr int BYTES = 2;
     static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ap_g_bf16x8, a), __builtin_bit_cast(ap_g_bf16x8, b), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ap_g_bf16x8, a), __builtin_bit_cast(ap_g_bf16x8, b), c, 0, 0, 0);
     }
 };
 struct ApF16Op {
-    typedef ap_g_f32x16 Acc;
+    typedef ap_g_f32x4 Acc;
     static constexpr int BYTES = 2;
     static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(ap_g_f16x8, a), __builtin_bit_cast(ap_g_f16x8, b), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ap_g_f16x8, a), __builtin_bit_cast(ap_g_f16x8, b), c, 0, 0, 0);
     }
 };
 struct ApI8Op {
-    typedef ap_g_i32x16 Acc;
+    typedef ap_g_i32x4 Acc;
     static constexpr int BYTES = 1;
-    static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 };
 
 #define AP_G_LINE 128   // bytes of k that a chunk takes of every row: 64 values of 16 bits, 128 of 8
@@ -64,19 +65,22 @@ __device__ __forceinline__ void ap_g_barrier() {
 }
 
 // A tile of TM x TN by WM x WN waves.
+// A tile of TM x TN by WM x WN waves.
 template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> struct ApGemm {
     static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
-    static constexpr int FA = TM / WM / 32, FB = TN / WN / 32;   // 32 x 32 blocks of a wave
+    static constexpr int FA = TM / WM / 16, FB = TN / WN / 16;   // 16 x 16 blocks of a wave
     static constexpr int A_BYTES = TM * AP_G_LINE, B_BYTES = TN * AP_G_LINE;
     static constexpr int STAGE = A_BYTES + B_BYTES, LDS_BYTES = 2 * STAGE;
     static constexpr int BK = AP_G_LINE / OP::BYTES;   // values of k in a chunk
+    static constexpr int STEPS = 2;                    // of 64 bytes of k
+    static constexpr int LA = TM / 8 / WAVES, LB = TN / 8 / WAVES;   // loads of a wave for a chunk, 1 KB each
     typedef typename OP::Acc Acc;
 
-    // Chunks of 16 bytes change places within a line of LDS, so that the lanes of one read fall in different banks.  Lines of k:
-    // 32 rows are read at the same chunk.  Lines of rows or columns: a read takes 32 columns of the lines k, k + 1, k + 2, k + 3,
-    // k + 8, .. k + 11.
-    static __device__ __forceinline__ int swap_k(int row) { return row & 7; }
-    static __device__ __forceinline__ int swap_t(int k, int t) { return (((k & 3) | ((k >> 1) & 4)) * 4) & (t * OP::BYTES / 16 - 1); }
+    // Chunks of 16 bytes change places within a line of LDS, so that the 16 lanes that are served at a time fall in different banks.  Lines of k: 16
+    // rows are read at the same chunk, and two rows fill the 256 bytes of all banks.  Lines of rows or columns: 32 lanes read 32 bytes of
+    // each of the lines k, .. k + 3, k + 8, .. k + 11.
+    static __device__ __forceinline__ int swap_k(int row) { return (row >> 1) & 7; }
+    static __device__ __forceinline__ int swap_t(int k, int t) { return (((k & 3) | ((k >> 1) & 4)) * 2) & (t * OP::BYTES / 16 - 1); }
 
     // The offsets, relative to a chunk's first byte, of what this lane brings of an operand of T rows.
     template <int T, bool LINE>
@@ -96,29 +100,28 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
     }
     // Loads a chunk's part of one operand; `left`: the bytes (K_LINE) or lines of k that are left from this chunk on.
     template <int T, bool LINE>
-    static __device__ __forceinline__ void load(const char *base, const uint32_t (&off)[T / 8 / WAVES], int32_t left, uint32_t lds, int wave, int lane) {
-        const bool whole = left >= (LINE ? AP_G_LINE : BK);
-#pragma unroll
-        for (int i = 0; i < T / 8 / WAVES; i++) {
-            uint32_t o = off[i];
-            if (!whole) {
-                const int at = (wave * (T / 8 / WAVES) + i) * 64 + lane;
-                const int place = LINE ? ((at & 7) ^ swap_k(at >> 3)) * 16 : at / (T * OP::BYTES / 16);
-                if (place >= left) o = 0x80000000u;
-            }
-            ap_g_load_lds(base, o, lds + (wave * (T / 8 / WAVES) + i) * 1024);
-        }
+    static __device__ __forceinline__ void load1(const char *base, const uint32_t (&off)[T / 8 / WAVES], int32_t left, uint32_t lds, int wave, int lane, int i) {
+        // where the lane's 16 bytes lie in the chunk: their byte of the line, or their line
+        constexpr int PER = T * OP::BYTES / 16;   // lanes of a line
+        const int place = LINE ? ((lane & 7) ^ swap_k((wave * (T / 8 / WAVES) + i) * 8 + (lane >> 3))) * 16 : lane / PER, before = LINE ? 0 : (wave * (T / 8 / WAVES) + i) * 64 / PER;
+        const uint32_t o = place < left - before ? off[i] : 0x80000000u;
+        ap_g_load_lds(base, o, lds + (wave * (T / 8 / WAVES) + i) * 1024);
     }
-    // The 16 bytes of k that this lane feeds to step `step` for the 32 rows from `row` on.
+    template <int T, bool LINE>
+    static __device__ __forceinline__ void load(const char *base, const uint32_t (&off)[T / 8 / WAVES], int32_t left, uint32_t lds, int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < T / 8 / WAVES; i++) load1<T, LINE>(base, off, left, lds, wave, lane, i);
+    }
+    // The 16 bytes of k that this lane feeds to step `step` for the 16 rows from `row` on: k from 16 (lane / 16) bytes on, of row lane % 16.
     template <int T, bool LINE>
     static __device__ __forceinline__ ap_g_i32x4 frag(const char *lds, int row, int step, int lane) {
         if (LINE) {
-            const int r = row + (lane & 31), chunk = (step * 2 + (lane >> 5)) ^ swap_k(r);
+            const int r = row + (lane & 15), chunk = (step * 4 + (lane >> 4)) ^ swap_k(r);
             return *reinterpret_cast<const ap_g_i32x4 *>(lds + r * AP_G_LINE + chunk * 16);
         } else {
             // 16 lanes read 4 lines of 16 columns and get 4 values of k of a column each
             static_assert(LINE || OP::BYTES == 2, "lines of rows are of 16-bit values");
-            const int g = lane >> 4, k = step * 16 + (g >> 1) * 8 + ((lane >> 2) & 3), col = (row + (g & 1) * 16 + (lane & 3) * 4) * 2;
+            const int k = step * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3), col = (row + (lane & 3) * 4) * 2;
             ap_g_s16x4 v[2];
 #pragma unroll
             for (int h = 0; h < 2; h++) {
@@ -145,57 +148,93 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
 #pragma unroll
             for (int b = 0; b < FB; b++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) acc[a][b][r] = 0;
+                for (int r = 0; r < 4; r++) acc[a][b][r] = 0;
         const int32_t per = (K + BK - 1) / BK, chunks = per * parts;
         const int64_t a_step = A_LINE ? AP_G_LINE : BK * A.ld, b_step = B_LINE ? AP_G_LINE : BK * B.ld;
         const uint32_t lds0 = (uint32_t)(uintptr_t)(AP_LDS char *)lds;
         const char *next_a = A.base + (parts > 1 ? a_part : 0), *next_b = B.base;   // of the next chunk to be brought
         int32_t left = K, part = 0;
-        auto bring = [&](int stage) {
-            const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
-            load<TM, A_LINE>(a, oa, A_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE, wave, lane);
-            load<TN, B_LINE>(b, ob, B_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE + A_BYTES, wave, lane);
+        auto advance = [&]() {
             next_a += a_step;
             next_b += b_step;
             left -= BK;
-            if (left <= 0 && ++part < parts) {
-                left = K;
+            if (left <= 0) {
+                part++;
+                left = part < parts ? K : 0;
                 next_a = A.base;
                 next_b = B.base + (part == 1 ? b_part : 0);
             }
         };
-        if (chunks > 0) bring(0);
-        for (int32_t c = 0; c < chunks; c++) {
-            ap_g_wait_loads<0>();
-            ap_g_barrier();   // chunk c is there, and nobody reads the other stage any more
-            if (c + 1 < chunks) bring((c + 1) & 1);
-            const char *sa = lds + (c & 1) * STAGE, *sb = sa + A_BYTES;
+        auto bring = [&](int stage) {
+            const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
+            load<TM, A_LINE>(a, oa, A_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE, wave, lane);
+            load<TN, B_LINE>(b, ob, B_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE + A_BYTES, wave, lane);
+            advance();
+        };
+        // A step's fragments are read while the step before is multiplied.  The barrier stands before the last step of a chunk: every wave has the
+        // chunk's last fragments in registers then, so its stage is filled again, and the next chunk has come.  The order is laid down
+        // (the compiler would put all reads before or behind the multiplications) and nothing in a chunk branches.
+        ap_g_i32x4 fr[2][FB + FA];
+        constexpr int NR = FA + FB, NM = FA * FB;
+        auto read1 = [&](int stage, int s, int to, int i) {
+            const char *sa = lds + stage * STAGE, *sb = sa + A_BYTES;
+            if (i < FB) fr[to][i] = frag<TN, B_LINE>(sb, wn * (TN / WN) + i * 16, s, lane);
+            else fr[to][i] = frag<TM, A_LINE>(sa, wm * (TM / WM) + (i - FB) * 16, s, lane);
+        };
+        auto mul = [&](int from, auto between) {
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
-                ap_g_i32x4 fa[FA], fb[FB];
-#pragma unroll
-                for (int a = 0; a < FA; a++) fa[a] = frag<TM, A_LINE>(sa, wm * (TM / WM) + a * 32, s, lane);
-#pragma unroll
-                for (int b = 0; b < FB; b++) fb[b] = frag<TN, B_LINE>(sb, wn * (TN / WN) + b * 32, s, lane);
-#pragma unroll
-                for (int a = 0; a < FA; a++)
-#pragma unroll
-                    for (int b = 0; b < FB; b++) acc[a][b] = OP::mul(fa[a], fb[b], acc[a][b]);
+            for (int i = 0; i < NM; i++) {
+                between(i);
+                __builtin_amdgcn_sched_barrier(0);
+                acc[i / FB][i % FB] = OP::mul(fr[from][FB + i / FB], fr[from][i % FB], acc[i / FB][i % FB]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        if (chunks > 0) {
+            bring(0);
+            ap_g_wait_loads<0>();
+            ap_g_barrier();
+            if (chunks > 1) bring(1);
+#pragma unroll
+            for (int i = 0; i < NR; i++) read1(0, 0, 0, i);
         }
+        for (int32_t c = 0; c < chunks; c++) {
+            const int st = c & 1;
+            mul(0, [&](int i) {   // the reads in the first half
+#pragma unroll
+                for (int r = min(NR, i * NR * 2 / NM); r < min(NR, (i + 1) * NR * 2 / NM); r++) read1(st, 1, 1, r);
+            });
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            ap_g_wait_loads<0>();
+            ap_g_barrier();
+            // past the last chunk nothing is left: the loads bring zeros that nobody reads
+            const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
+            const int32_t la = ap_uniform_i32(A_LINE ? left * OP::BYTES : left), lb = ap_uniform_i32(B_LINE ? left * OP::BYTES : left);
+            mul(1, [&](int i) {
+#pragma unroll
+                for (int r = min(NR, i * NR * 2 / NM); r < min(NR, (i + 1) * NR * 2 / NM); r++) read1(st ^ 1, 0, 0, r);
+#pragma unroll
+                for (int l = i * (LA + LB) / NM; l < (i + 1) * (LA + LB) / NM; l++) {
+                    if (l < LA) load1<TM, A_LINE>(a, oa, la, lds0 + st * STAGE, wave, lane, l);
+                    else load1<TN, B_LINE>(b, ob, lb, lds0 + st * STAGE + A_BYTES, wave, lane, l - LA);
+                }
+            });
+            advance();
+        }
+        ap_g_wait_loads<0>();
         ap_g_barrier();   // the stages may be used for something else
     }
+    // Where element r of this lane's block (a, b) lies: row(a) + r, col(b).
+    static __device__ __forceinline__ int row(int a) { return ap_wave_id() / WN * (TM / WM) + a * 16 + 4 * ((threadIdx.x & 63) >> 4); }
+    static __device__ __forceinline__ int col(int b) { return ap_wave_id() % WN * (TN / WN) + b * 16 + (threadIdx.x & 15); }
     // Calls f(i, j, value) for every element that this lane holds of the tile.
     template <class F> static __device__ __forceinline__ void each(const Acc (&acc)[FA][FB], F f) {
-        const int lane = threadIdx.x & 63, wave = ap_wave_id();
-        const int wm = wave / WN, wn = wave % WN;
 #pragma unroll
         for (int a = 0; a < FA; a++)
 #pragma unroll
             for (int b = 0; b < FB; b++)
 #pragma unroll
-                for (int r = 0; r < 16; r++)
-                    f(wm * (TM / WM) + a * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), wn * (TN / WN) + b * 32 + (lane & 31), acc[a][b][r]);
+                for (int r = 0; r < 4; r++) f(row(a) + r, col(b), acc[a][b][r]);
     }
 };
 

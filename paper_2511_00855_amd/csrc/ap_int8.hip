@@ -111,23 +111,33 @@ __global__ __launch_bounds__(WM *WN * 64) void k_scores8(ApScores8 p) {
     const int32_t m0 = mt * TM, n0 = nt * TN, queries = min(TM, p.rows - m0), docs = min(TN, p.n - n0);
     typename G::Acc acc[G::FA][G::FB];
     G::product({p.x + m0 * p.ldx, p.ldx, queries}, {p.q + n0 * p.ldq, p.ldq, docs}, p.pad, 1, 0, 0, lds, acc);
-    const int lane = threadIdx.x & 63, wave = ap_wave_id(), wm = wave / WN, wn = wave % WN;
-    const int row0 = wm * (TM / WM) + 4 * (lane >> 5), col0 = wn * (TN / WN) + (lane & 31);
-    float sd[G::FB];
+    // all scales first: a load between the stores would wait for them
+    float sd[G::FB], sx[G::FA][4];
 #pragma unroll
-    for (int b = 0; b < G::FB; b++) sd[b] = col0 + b * 32 < docs ? p.q_scale[n0 + col0 + b * 32] : 0.f;
+    for (int b = 0; b < G::FB; b++) sd[b] = G::col(b) < docs ? p.q_scale[n0 + G::col(b)] : 0.f;
 #pragma unroll
     for (int a = 0; a < G::FA; a++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            const int i = row0 + a * 32 + 8 * (r >> 2) + (r & 3);
-            if (i >= queries) continue;
-            const float sx = p.x_scale[m0 + i];
-            float *to = p.out + (int64_t)(m0 + i) * p.ld_out + n0 + col0;
+        for (int r = 0; r < 4; r++) sx[a][r] = p.x_scale[m0 + min(G::row(a) + r, queries - 1)];
+    float *out = p.out + (int64_t)m0 * p.ld_out + n0;
+    if (queries == TM && docs == TN) {
+#pragma unroll
+        for (int a = 0; a < G::FA; a++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                float *to = out + (G::row(a) + r) * p.ld_out;
+#pragma unroll
+                for (int b = 0; b < G::FB; b++) to[G::col(b)] = (float)acc[a][b][r] * sx[a][r] * sd[b];
+            }
+        return;
+    }
+#pragma unroll
+    for (int a = 0; a < G::FA; a++)
+#pragma unroll
+        for (int r = 0; r < 4; r++)
 #pragma unroll
             for (int b = 0; b < G::FB; b++)
-                if (col0 + b * 32 < docs) to[b * 32] = (float)acc[a][b][r] * sx * sd[b];
-        }
+                if (G::row(a) + r < queries && G::col(b) < docs) out[(G::row(a) + r) * p.ld_out + G::col(b)] = (float)acc[a][b][r] * sx[a][r] * sd[b];
 }
 
 // ------------------------------------------------------------------ host side

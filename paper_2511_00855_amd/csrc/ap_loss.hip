@@ -25,20 +25,40 @@
 // ------------------------------------------------------------------ f32 rows as two f16 parts
 // Largest finite magnitude of two arrays of rows, as the bits of a float (which are in the order of the numbers).
 struct ApSide { const float *p; int64_t ld, rows; };
+// Four 16-byte groups of a matrix of `total` at once: group i + k * step of it, or nothing past the end.
+__device__ __forceinline__ void ap_load4(const ApSide &s, int32_t per, int64_t total, int64_t i, int64_t step, float4 (&v)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int64_t at = i + k * step;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at < total) v[k] = *reinterpret_cast<const float4 *>(s.p + (s.ld == per * 4 ? at * 4 : at / per * s.ld + at % per * 4));
+    }
+}
 __global__ __launch_bounds__(256) void k_loss_amax(ApSide a, ApSide b, int32_t dim, uint32_t *__restrict__ out /* [2], zero */) {
+    __shared__ float s_m[4];
     const int32_t per = dim / 4;
     for (int side = 0; side < 2; side++) {
         const ApSide s = side ? b : a;
+        const int64_t total = s.rows * per, step = (int64_t)gridDim.x * 256;
         float m = 0.f;
-        for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < s.rows; r += (int64_t)gridDim.x * 4)
-            for (int32_t c = threadIdx.x & 63; c < per; c += 64) {
-                const float4 v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c * 4);
-                const float x[4] = {fabsf(v.x), fabsf(v.y), fabsf(v.z), fabsf(v.w)};
+        for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += 4 * step) {
+            float4 v[4];
+            ap_load4(s, per, total, i, step, v);
 #pragma unroll
-                for (int i = 0; i < 4; i++) m = x[i] > m && x[i] < INFINITY ? x[i] : m;
+            for (int k = 0; k < 4; k++) {
+                const float x[4] = {fabsf(v[k].x), fabsf(v[k].y), fabsf(v[k].z), fabsf(v[k].w)};
+#pragma unroll
+                for (int j = 0; j < 4; j++) m = x[j] > m && x[j] < INFINITY ? x[j] : m;
             }
+        }
         for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        if ((threadIdx.x & 63) == 0 && m > 0.f) atomicMax(&out[side], __float_as_uint(m));
+        if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
+        __syncthreads();
+        if (threadIdx.x == 0) {   // one atomic a block, and none that would change nothing: thousands on one address cost as much as the reads
+            m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+            if (__float_as_uint(m) > *(volatile uint32_t *)&out[side]) atomicMax(&out[side], __float_as_uint(m));
+        }
+        __syncthreads();
     }
 }
 // The power of two that brings a largest magnitude into [2^14, 2^15).
@@ -49,22 +69,22 @@ __global__ __launch_bounds__(256) void k_loss_split(ApSide s, int32_t dim, int32
                                                     _Float16 *__restrict__ hi, _Float16 *__restrict__ lo) {
     const int up = ap_loss_up(*amax);
     const int32_t per = pad / 4;
-    for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < s.rows; r += (int64_t)gridDim.x * 4) {
-        const bool used = !coef || coef[r] != 0.f;
-        for (int32_t c = threadIdx.x & 63; c < per; c += 64) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (used && c * 4 < dim) v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c * 4);
-            const float x[4] = {v.x, v.y, v.z, v.w};
-            _Float16 h[4], l[4];
+    const int64_t total = s.rows * per, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += step) {
+        const int64_t r = i / per;
+        const int32_t c = (int32_t)(i - r * per) * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < dim && (!coef || coef[r] != 0.f)) v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c);
+        const float x[4] = {v.x, v.y, v.z, v.w};
+        _Float16 h[4], l[4];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float y = ldexpf(x[i], up);
-                h[i] = (_Float16)y;
-                l[i] = (_Float16)(y - (float)h[i]);
-            }
-            *reinterpret_cast<uint2 *>(hi + r * pad + c * 4) = *reinterpret_cast<const uint2 *>(h);
-            *reinterpret_cast<uint2 *>(lo + r * pad + c * 4) = *reinterpret_cast<const uint2 *>(l);
+        for (int j = 0; j < 4; j++) {
+            const float y = ldexpf(x[j], up);
+            h[j] = (_Float16)y;
+            l[j] = (_Float16)(y - (float)h[j]);
         }
+        *reinterpret_cast<uint2 *>(hi + i * 4) = *reinterpret_cast<const uint2 *>(h);
+        *reinterpret_cast<uint2 *>(lo + i * 4) = *reinterpret_cast<const uint2 *>(l);
     }
 }
 
@@ -110,38 +130,30 @@ template <bool PARTS> __device__ __forceinline__ void ap_lse_join(float &m, floa
     m = t;
 }
 
-// Coefficients of four documents in a row of one query: v are the logits times log2(e), g its weight (0: none), `at` where its label lies from
-// the first on, `docs` how many of them there are.
+// A coefficient out of a logit times log2(e), for a query of weight g (0: none).
 struct ApCoef {
     float g, lse2, lse2_lo;
     __device__ __forceinline__ ApCoef(float g_, float lse) : g(g_), lse2(lse * AP_LOG2E) { lse2_lo = fmaf(lse, AP_LOG2E, -lse2) + lse * AP_LOG2E_LO; }
-    template <bool PARTS> __device__ __forceinline__ void put(const float *v, int64_t at, int64_t docs, char *to, int64_t c_part) const {
-        float c[4];
+    __device__ __forceinline__ float exp_of(float v) const { return __builtin_amdgcn_exp2f((v - lse2) - lse2_lo); }
+    __device__ __forceinline__ float times(float e) const { return g != 0.f ? e * g : 0.f; }   // e: the exponential, less 1 at the label
+};
+// Four coefficients as 16-bit numbers (f16: times 2^AP_COEF_UP); what they are off by stays in v.
+template <bool F16> __device__ __forceinline__ uint2 ap_coef_part(float (&v)[4]) {
+    if (F16) {
+        _Float16 h[4];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            float e = __builtin_amdgcn_exp2f((v[i] - lse2) - lse2_lo);
-            if (at == i) e -= 1.f;
-            c[i] = g != 0.f && i < docs ? e * g : 0.f;
+            const float y = v[i] * (float)(1 << AP_COEF_UP);
+            h[i] = (_Float16)y;
+            v[i] = (y - (float)h[i]) * (1.f / (float)(1 << AP_COEF_UP));
         }
-        if (PARTS) {
-            _Float16 h[4], l[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float y = ldexpf(c[i], AP_COEF_UP);
-                h[i] = (_Float16)y;
-                l[i] = (_Float16)(y - (float)h[i]);
-            }
-            *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(h);
-            *reinterpret_cast<uint2 *>(to + c_part) = *reinterpret_cast<const uint2 *>(l);
-        } else {
-            const uint2 h = make_uint2(ap_bf16_pair(c[0], c[1]), ap_bf16_pair(c[2], c[3]));
-            *reinterpret_cast<uint2 *>(to) = h;
-            if (c_part)
-                *reinterpret_cast<uint2 *>(to + c_part) = make_uint2(ap_bf16_pair(c[0] - __uint_as_float(h.x << 16), c[1] - __uint_as_float(h.x & 0xffff0000u)),
-                                                                     ap_bf16_pair(c[2] - __uint_as_float(h.y << 16), c[3] - __uint_as_float(h.y & 0xffff0000u)));
-        }
+        return *reinterpret_cast<const uint2 *>(h);
     }
-};
+    const uint2 h = make_uint2(ap_bf16_pair(v[0], v[1]), ap_bf16_pair(v[2], v[3]));
+    v[0] -= __uint_as_float(h.x << 16); v[1] -= __uint_as_float(h.x & 0xffff0000u);
+    v[2] -= __uint_as_float(h.y << 16); v[3] -= __uint_as_float(h.y & 0xffff0000u);
+    return h;
+}
 
 // GRAD: the tile's coefficients.  Otherwise its maximum and sum a query.
 template <class OP, int TM, int TN, int WM, int WN, bool PARTS, bool GRAD>
@@ -155,55 +167,92 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
     typename G::Acc acc[G::FA][G::FB];
     G::product({p.docs + (p.first + m0) * p.ldd, p.ldd, docs}, {p.x + n0 * p.ldx, p.ldx, queries}, p.dim, PARTS ? 3 : 1, p.d_part, p.x_part, lds, acc);
 
-    const int lane = threadIdx.x & 63, wave = ap_wave_id(), wm = wave / WN, wn = wave % WN;
+    const int lane = threadIdx.x & 63, wm = ap_wave_id() / WN, row0 = G::row(0);   // a lane's rows: row0 + 16 a + r
     const ApFactor f(p.scale, PARTS ? p.amax : nullptr);
-    const int row0 = wm * (TM / WM) + 4 * (lane >> 5);   // of block a, register r: row0 + 32 a + 8 (r / 4) + r % 4
     float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + WM * TN;
 #pragma unroll
     for (int b = 0; b < G::FB; b++) {
-        const int col = wn * (TN / WN) + b * 32 + (lane & 31);
+        const int col = G::col(b);
         const bool is = col < queries;
         const int32_t label = is ? p.labels[n0 + col] : -1;
         const int64_t local = (int64_t)label - p.first - m0 - row0;   // of the label among this lane's rows
         if (!GRAD) {
-            if (label >= 0 && local >= 0 && local < TM / WM && !(local & 4)) {
+            if (label >= 0 && local >= 0 && local < TM / WM && !(local & 12)) {
 #pragma unroll
                 for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                    for (int r = 0; r < 16; r++)
-                        if (local == a * 32 + 8 * (r >> 2) + (r & 3) && local + row0 < docs) p.at_label[n0 + col] = acc[a][b][r];
+                    for (int r = 0; r < 4; r++)
+                        if (local == a * 16 + r && local + row0 < docs) p.at_label[n0 + col] = acc[a][b][r];
             }
             if (docs < TM)
 #pragma unroll
                 for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                    for (int r = 0; r < 16; r++)
-                        if (row0 + a * 32 + 8 * (r >> 2) + (r & 3) >= docs) acc[a][b][r] = -INFINITY;
+                    for (int r = 0; r < 4; r++)
+                        if (row0 + a * 16 + r >= docs) acc[a][b][r] = -INFINITY;
             float m = -INFINITY;
 #pragma unroll
             for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) m = fmaxf(m, acc[a][b][r]);
+                for (int r = 0; r < 4; r++) m = fmaxf(m, acc[a][b][r]);
+            m = fmaxf(m, __shfl_xor(m, 16, 64));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
             const float base = m == -INFINITY ? 0.f : m;
             float s = 0.f;
 #pragma unroll
             for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                for (int r = 0; r < 16; r++) s += __builtin_amdgcn_exp2f(f.of<PARTS>(acc[a][b][r] - base));
+                for (int r = 0; r < 4; r++) s += __builtin_amdgcn_exp2f(f.of<PARTS>(acc[a][b][r] - base));
+            s += __shfl_xor(s, 16, 64);
             s += __shfl_xor(s, 32, 64);
-            if (lane < 32) { s_max[wm * TN + col] = m; s_sum[wm * TN + col] = s; }
+            if (lane < 16) { s_max[wm * TN + col] = m; s_sum[wm * TN + col] = s; }
         } else {
             const ApCoef coef(is ? p.coef[n0 + col] : 0.f, is ? p.lse[n0 + col] : 0.f);
-            char *to = p.c + (int64_t)(n0 + col) * p.ldc + (m0 + row0) * 2;
 #pragma unroll
             for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const int at = a * 32 + 2 * r;
-                    const float v[4] = {f.of<PARTS>(acc[a][b][r]), f.of<PARTS>(acc[a][b][r + 1]), f.of<PARTS>(acc[a][b][r + 2]), f.of<PARTS>(acc[a][b][r + 3])};
-                    if (is) coef.put<PARTS>(v, local - at, docs - row0 - at, to + at * 2, p.c_part);
+                for (int r = 0; r < 4; r++) acc[a][b][r] = coef.exp_of(f.of<PARTS>(acc[a][b][r]));
+            if (local >= 0 && local < TM / WM && !(local & 12)) {
+#pragma unroll
+                for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+                        if (local == a * 16 + r) acc[a][b][r] -= 1.f;
+            }
+#pragma unroll
+            for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) acc[a][b][r] = coef.times(acc[a][b][r]);
+            if (docs < TM)
+#pragma unroll
+                for (int a = 0; a < G::FA; a++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++)
+                        if (row0 + a * 16 + r >= docs) acc[a][b][r] = 0.f;
+        }
+    }
+    if (GRAD) {
+        // a part of the coefficients goes through LDS, a query's documents together, and leaves in whole lines (four documents of a lane at a time
+        // would write 32 bytes of 16 lines: a tile of 256 took half as long again); groups of 16 bytes change places by the query
+        constexpr int LINE = TM * 2, GROUPS = LINE / 16;
+        for (int part = 0; part < (p.c_part ? 2 : 1); part++) {
+#pragma unroll
+            for (int b = 0; b < G::FB; b++)
+#pragma unroll
+                for (int a = 0; a < G::FA; a++) {
+                    const int col = G::col(b), at = (row0 + a * 16) * 2, group = (at >> 4) ^ (col & (GROUPS < 16 ? GROUPS - 1 : 15));
+                    float v[4] = {acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]};
+                    *reinterpret_cast<uint2 *>(lds + col * LINE + group * 16 + (at & 15)) = ap_coef_part<PARTS>(v);
+#pragma unroll
+                    for (int r = 0; r < 4; r++) acc[a][b][r] = v[r];   // what is left for the second part
                 }
+            __syncthreads();
+            for (int i = threadIdx.x; i < queries * GROUPS; i += G::THREADS) {
+                const int q = i / GROUPS, group = i % GROUPS;
+                *reinterpret_cast<uint4 *>(p.c + part * p.c_part + (int64_t)(n0 + q) * p.ldc + m0 * 2 + group * 16) =
+                    *reinterpret_cast<const uint4 *>(lds + q * LINE + (group ^ (q & (GROUPS < 16 ? GROUPS - 1 : 15))) * 16);
+            }
+            __syncthreads();
         }
     }
     if (!GRAD) {
@@ -225,9 +274,15 @@ __global__ __launch_bounds__(1024) void k_loss_join(const float2 *__restrict__ p
     const int32_t q = (blockIdx.x << qb) + (threadIdx.x & ((1 << qb) - 1));
     float m = -INFINITY, s = 0.f;
     if (q < rows)
-        for (int64_t t = threadIdx.x >> qb; t < tiles; t += 1024 >> qb) {
-            const float2 v = part[t * rows + q];
-            ap_lse_join<true>(m, s, v.x, v.y, f);
+        for (int64_t t = threadIdx.x >> qb; t < tiles; t += 4 * (1024 >> qb)) {
+            float2 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int64_t at = t + k * (1024 >> qb);
+                v[k] = at < tiles ? part[at * rows + q] : make_float2(-INFINITY, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k++) ap_lse_join<true>(m, s, v[k].x, v[k].y, f);
         }
     s_m[threadIdx.x] = m;
     s_s[threadIdx.x] = s;
@@ -285,8 +340,16 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
             for (int g = 0; g < NQ; g++) {
                 const int q = g * 16 + (lane & 15);
                 if (q >= p.rows) continue;
-                const float v[4] = {f.of<false>(acc[g][0]), f.of<false>(acc[g][1]), f.of<false>(acc[g][2]), f.of<false>(acc[g][3])};
-                ApCoef(coef[g], lse[g]).put<DT == AP_F32>(v, label[g] - p.first - d, p.count - d, p.c + q * p.ldc + d * 2, p.c_part);
+                const ApCoef co(coef[g], lse[g]);
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const float e = co.exp_of(f.of<false>(acc[g][r])) - (label[g] == p.first + d + r ? 1.f : 0.f);
+                    v[r] = d + r < p.count ? co.times(e) : 0.f;
+                }
+                char *to = p.c + q * p.ldc + d * 2;
+                *reinterpret_cast<uint2 *>(to) = ap_coef_part<DT == AP_F32>(v);
+                if (p.c_part) *reinterpret_cast<uint2 *>(to + p.c_part) = ap_coef_part<DT == AP_F32>(v);
             }
         });
         return;
@@ -366,9 +429,9 @@ struct ApLossGrad {
     const float *most;
     void *grad_docs;               // NULL: not wanted
     int64_t ld_out;
-    float *gx;                     // NULL: not wanted; [split][query][dim], sums so far
-    int32_t splits, split_docs;    // the documents of the piece in `splits` runs of `split_docs`
-    int32_t tiles_docs;            // workgroups of the documents' gradient; the others make the queries'
+    float *gx;                     // [run][query][dim], sums so far
+    uint32_t runs;                 // the queries' gradient (0: not wanted) takes the documents of the piece in as many runs
+    int32_t run_docs;
     int32_t parts;                 // pairs of parts that are multiplied: 1, 2 (two parts of the coefficients), 3 (of both factors)
     int32_t start;                 // 1: first piece, nothing is there to add to
 };
@@ -378,34 +441,34 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
     using GD = ApGemm<OP, TM, TN, WM, WN, false, false>;
     using GX = ApGemm<OP, TM, TN, WM, WN, true, false>;
     __shared__ __attribute__((aligned(1024))) char lds[GD::LDS_BYTES];
-    const uint32_t nt = (p.dim + TN - 1) / TN;
+    const uint32_t mt = (p.rows + TM - 1) / TM, nt = (p.dim + TN - 1) / TN;
     typename GD::Acc acc[GD::FA][GD::FB];
-    if ((int32_t)blockIdx.x < p.tiles_docs) {
+    if (blockIdx.x < p.runs * mt * nt) {   // the longer ones first
         uint32_t m, n;
-        ap_g_tile(blockIdx.x, (p.count + TM - 1) / TM, nt, nt, &m, &n);
-        const int32_t m0 = m * TM, n0 = n * TN, docs = min(TM, p.count - m0), cols = min(TN, p.dim - n0);
-        GD::product({p.c + m0 * 2, p.ldc, docs * 2}, {p.x + n0 * 2, p.ldx, cols * 2}, p.rows, p.parts, p.c_part, p.x_part, lds, acc);
-        float f1 = p.scale, f2 = *p.most;
-        if (PARTS) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(p.amax[1])); }
-        const int64_t at0 = (p.first + m0) * p.ld_out + n0;
-        GD::each(acc, [&](int i, int j, float v) {
-            if (i >= docs || j >= cols) return;
-            v = v * f1 * f2;
-            if (PARTS) static_cast<float *>(p.grad_docs)[at0 + i * p.ld_out + j] = v;
-            else static_cast<__bf16 *>(p.grad_docs)[at0 + i * p.ld_out + j] = (__bf16)v;
-        });
+        ap_g_tile(blockIdx.x, p.runs * mt, nt, nt, &m, &n);
+        const uint32_t run = m / mt, m0 = m % mt * TM, n0 = n * TN;
+        const int32_t queries = min(TM, p.rows - (int32_t)m0), cols = min(TN, p.dim - (int32_t)n0);
+        const int64_t d0 = (int64_t)run * p.run_docs, docs = min((int64_t)p.run_docs, p.count - d0);
+        GX::product({p.c + m0 * p.ldc + d0 * 2, p.ldc, queries}, {p.docs + (p.first + d0) * p.ldd + n0 * 2, p.ldd, cols * 2}, docs > 0 ? docs : 0, p.parts, p.c_part, p.d_part, lds, acc);
+        float *to = p.gx + ((int64_t)run * p.rows + m0) * p.dim + n0;
+        // One workgroup of a launch adds to an element, and launches follow each other: the sums have one order, atomics or not.  They save the wait for
+        // what is there.
+        if (p.start) GX::each(acc, [&](int i, int j, float v) { if (i < queries && j < cols) to[(int64_t)i * p.dim + j] = v; });
+        else GX::each(acc, [&](int i, int j, float v) { if (i < queries && j < cols) unsafeAtomicAdd(to + (int64_t)i * p.dim + j, v); });
         return;
     }
-    const uint32_t mt = (p.rows + TM - 1) / TM, block = blockIdx.x - p.tiles_docs;
-    const uint32_t split = block / (mt * nt), t = block % (mt * nt), m0 = t / nt * TM, n0 = t % nt * TN;
-    const int32_t queries = min(TM, p.rows - (int32_t)m0), cols = min(TN, p.dim - (int32_t)n0);
-    const int64_t d0 = (int64_t)split * p.split_docs, docs = min((int64_t)p.split_docs, p.count - d0);
-    GX::product({p.c + m0 * p.ldc + d0 * 2, p.ldc, queries}, {p.docs + (p.first + d0) * p.ldd + n0 * 2, p.ldd, cols * 2}, docs > 0 ? docs : 0, p.parts, p.c_part, p.d_part, lds, acc);
-    float *to = p.gx + ((int64_t)split * p.rows + m0) * p.dim + n0;
-    GX::each(acc, [&](int i, int j, float v) {
-        if (i >= queries || j >= cols) return;
-        float *at = to + (int64_t)i * p.dim + j;
-        *at = p.start ? v : *at + v;
+    uint32_t m, n;
+    ap_g_tile(blockIdx.x - p.runs * mt * nt, (p.count + TM - 1) / TM, nt, nt, &m, &n);
+    const int32_t m0 = m * TM, n0 = n * TN, docs = min(TM, p.count - m0), cols = min(TN, p.dim - n0);
+    GD::product({p.c + m0 * 2, p.ldc, docs * 2}, {p.x + n0 * 2, p.ldx, cols * 2}, p.rows, p.parts, p.c_part, p.x_part, lds, acc);
+    float f1 = p.scale, f2 = *p.most;
+    if (PARTS) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(p.amax[1])); }
+    const int64_t at0 = (p.first + m0) * p.ld_out + n0;
+    GD::each(acc, [&](int i, int j, float v) {
+        if (i >= docs || j >= cols) return;
+        v = v * f1 * f2;
+        if (PARTS) static_cast<float *>(p.grad_docs)[at0 + i * p.ld_out + j] = v;
+        else static_cast<__bf16 *>(p.grad_docs)[at0 + i * p.ld_out + j] = (__bf16)v;
     });
 }
 
@@ -478,9 +541,9 @@ struct LossParts {   // f32 rows as two f16 parts
     int make(const void *xp, int64_t ldx, int64_t rows, const void *dp, int64_t ldd, int64_t n, int32_t dim, const float *coef, hipStream_t st) {
         const ApSide sd = {static_cast<const float *>(dp), ldd, n}, sx = {static_cast<const float *>(xp), ldx, rows};
         AP_TRY(ap_fill_u32(amax, 2, 0, st));
-        hipLaunchKernelGGL(k_loss_amax, dim3((unsigned)std::min<int64_t>(div_up(n, 4), 2048)), dim3(256), 0, st, sd, sx, dim, amax);
-        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(n, 4), 4096)), dim3(256), 0, st, sd, dim, (int32_t)pad, amax, nullptr, docs, docs + n * pad);
-        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(rows, 4), 4096)), dim3(256), 0, st, sx, dim, (int32_t)pad, amax + 1, coef, x, x + rows * pad);
+        hipLaunchKernelGGL(k_loss_amax, dim3((unsigned)std::min<int64_t>(div_up(n * (dim / 4), 1024), 2048)), dim3(256), 0, st, sd, sx, dim, amax);
+        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(n * (pad / 4), 256), 16384)), dim3(256), 0, st, sd, dim, (int32_t)pad, amax, nullptr, docs, docs + n * pad);
+        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(rows * (pad / 4), 256), 16384)), dim3(256), 0, st, sx, dim, (int32_t)pad, amax + 1, coef, x, x + rows * pad);
         AP_CHECK_HIP(hipGetLastError());
         return AP_OK;
     }
@@ -582,7 +645,7 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
         AP_TRY((launch_tiles<ApBf16Op, false, false>(p, plan.tile, st)));
     }
     int qb = 0;
-    while (qb < 6 && (1 << qb) < rows) qb++;
+    while (qb < 4 && (1 << qb) < rows) qb++;   // 16 queries a block: 128 bytes of pairs together, and enough blocks
     hipLaunchKernelGGL(k_loss_join, dim3((unsigned)div_up(rows, 1 << qb)), dim3(1024), 0, st, plan.part, plan.pairs, (int32_t)rows, qb, labels, (int32_t)n,
                        plan.at_label, scale, p.amax, loss, lse);
     AP_CHECK_HIP(hipGetLastError());
@@ -591,11 +654,32 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
 
 #define AP_LOSS_PIECE_BYTES ((int64_t)128 << 20)   // of the coefficients of a piece, one part: they stay in the last cache until they are multiplied
 
+// In how many runs of its documents the queries' gradient is made, so that its workgroups (`tiles` a run, taken first) and the `more` of the documents'
+// gradient, `k` long, end together on 256 compute units.  A workgroup costs its length and about 512 for its start and end.
+static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k) {
+    const int64_t cus = 256, over = 512;
+    int32_t best = 1;
+    int64_t least = INT64_MAX;
+    for (int32_t s = 1; s <= 64 && (s == 1 || piece / s >= 256); s++) {
+        const int64_t a = div_up(piece, s) + over, b = k + over, full = tiles * s / cus, late = tiles * s % cus;   // `late` units are busy for one more
+        const int64_t t0 = full * a, t1 = late ? t0 + a : t0;
+        // the first time by which the units that are free take all of the others
+        int64_t lo = t1, hi = t1 + div_up(more, cus) * b + b;
+        while (lo < hi) {
+            const int64_t t = (lo + hi) / 2;
+            if ((cus - late) * ((t - t0) / b) + late * ((t - t1) / b) >= more) hi = t; else lo = t + 1;
+        }
+        const int64_t cost = lo + s * over / 16;   // every run is added up once more at the end
+        if (cost < least) { least = cost; best = s; }
+    }
+    return best;
+}
+
 struct GradPlan {
     int64_t piece, ldc, c_part;
     int tile_c, tile;
     bool few, two;
-    int32_t splits, split_docs;
+    int32_t runs, run_docs;
     float *most, *coef, *gx;
     char *c, *x;
     LossParts parts;
@@ -615,16 +699,13 @@ struct GradPlan {
         tile = pick_tile(piece, dim);
         if (tile > 128 && r <= 128) tile = 128;
         if (tile > 64 && r <= 64) tile = 64;
-        // the queries' gradient: as much work a workgroup as the documents' has, and no fewer workgroups than fill the compute units
-        const int64_t tiles = div_up(r, tile) * div_up(dim, tile);
-        const int64_t by_work = div_up(piece, std::max<int64_t>(r, 512)), by_cus = div_up(256, tiles);
-        splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>({std::max(by_work, by_cus), div_up(piece, 256), 64}));
-        split_docs = (int32_t)up_to(div_up(piece, splits), 64);
-        splits = (int32_t)div_up(piece, split_docs);
+        runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r);
+        run_docs = (int32_t)up_to(div_up(piece, runs), 64);
+        runs = (int32_t)div_up(piece, run_docs);
         most = ws.take<float>(1);
         coef = ws.take<float>(r);
         c = ws.take<char>(c_part * (dtype == AP_F32 || two ? 2 : 1));
-        gx = want_x ? ws.take<float>(splits * r * dim) : nullptr;
+        gx = want_x ? ws.take<float>(runs * r * dim) : nullptr;
         if (dtype == AP_F32) parts.take(ws, r, n, dim);
         else x = ws.take<char>(r * dim * 2);
         return ws.bytes;
@@ -652,13 +733,11 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, const ApLoss &few, ApLoss
             AP_TRY((launch_tiles<OP, PARTS, true>(p, plan.tile_c, st)));
         }
         const int64_t nt = div_up(g.dim, plan.tile);
-        g.tiles_docs = g.grad_docs ? (int32_t)(div_up(g.count, plan.tile) * nt) : 0;
-        g.splits = plan.splits;
-        g.split_docs = plan.split_docs;
+        g.run_docs = plan.run_docs;
         g.start = d0 == 0;
         // a short last piece leaves the runs past its end alone
-        const int64_t runs = g.start ? plan.splits : div_up(g.count, plan.split_docs);
-        const dim3 grid((unsigned)(g.tiles_docs + (g.gx ? runs * div_up(g.rows, plan.tile) * nt : 0)));
+        g.runs = (uint32_t)(!g.gx ? 0 : g.start ? plan.runs : div_up(g.count, plan.run_docs));
+        const dim3 grid((unsigned)(g.runs * div_up(g.rows, plan.tile) * nt + (g.grad_docs ? div_up(g.count, plan.tile) * nt : 0)));
         if (plan.tile == 256) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
         else if (plan.tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         else hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
@@ -699,13 +778,13 @@ extern "C" int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, co
         p.docs = g.docs = (const char *)q.docs; p.x = g.x = (const char *)q.x; p.ldd = p.ldx = g.ldd = g.ldx = q.pad * 2;
         p.d_part = g.d_part = q.d_part; p.x_part = g.x_part = q.x_part; p.amax = g.amax = q.amax; p.dim = (int32_t)q.pad;
         AP_TRY((loss_pieces<ApF16Op, true>(plan, p, few, g, n, st)));
-        if (grad_x) hipLaunchKernelGGL((k_loss_gx<false>), dim3(join), dim3(256), 0, st, plan.gx, plan.splits, (int32_t)rows, dim, scale, plan.most, q.amax, grad_x, (int64_t)dim);
+        if (grad_x) hipLaunchKernelGGL((k_loss_gx<false>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, q.amax, grad_x, (int64_t)dim);
     } else {
         hipLaunchKernelGGL(k_loss_used, dim3((unsigned)std::min<int64_t>(div_up(rows * dim / 8, 256), 4096)), dim3(256), 0, st, static_cast<const char *>(x), ldx * 2, (int32_t)rows,
                            dim / 8, plan.coef, reinterpret_cast<uint4 *>(plan.x));
         p.docs = g.docs = static_cast<const char *>(docs); p.x = g.x = plan.x; p.ldd = g.ldd = ldd * 2; p.ldx = g.ldx = (int64_t)dim * 2; p.dim = dim;
         AP_TRY((loss_pieces<ApBf16Op, false>(plan, p, few, g, n, st)));
-        if (grad_x) hipLaunchKernelGGL((k_loss_gx<true>), dim3(join), dim3(256), 0, st, plan.gx, plan.splits, (int32_t)rows, dim, scale, plan.most, nullptr, grad_x, (int64_t)dim);
+        if (grad_x) hipLaunchKernelGGL((k_loss_gx<true>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, nullptr, grad_x, (int64_t)dim);
     }
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
