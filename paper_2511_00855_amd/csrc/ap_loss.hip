@@ -467,8 +467,8 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
     GD::each(acc, [&](int i, int j, float v) {
         if (i >= docs || j >= cols) return;
         v = v * f1 * f2;
-        if (PARTS) static_cast<float *>(p.grad_docs)[at0 + i * p.ld_out + j] = v;
-        else static_cast<__bf16 *>(p.grad_docs)[at0 + i * p.ld_out + j] = (__bf16)v;
+        if (PARTS) __builtin_nontemporal_store(v, static_cast<float *>(p.grad_docs) + at0 + i * p.ld_out + j);
+        else __builtin_nontemporal_store((__bf16)v, static_cast<__bf16 *>(p.grad_docs) + at0 + i * p.ld_out + j);
     });
 }
 
@@ -656,12 +656,12 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
 
 // In how many runs of its documents the queries' gradient is made, so that its workgroups (`tiles` a run, taken first) and the `more` of the documents'
 // gradient, `k` long, end together on 256 compute units.  A workgroup costs its length and about 512 for its start and end.
-static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k) {
+static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k, int64_t parts, int64_t *cost_of = nullptr) {
     const int64_t cus = 256, over = 512;
     int32_t best = 1;
     int64_t least = INT64_MAX;
-    for (int32_t s = 1; s <= 64 && (s == 1 || piece / s >= 256); s++) {
-        const int64_t a = div_up(piece, s) + over, b = k + over, full = tiles * s / cus, late = tiles * s % cus;   // `late` units are busy for one more
+    for (int32_t s = 1; s <= 32 && (s == 1 || piece / s >= 256); s++) {
+        const int64_t a = div_up(piece, s) * parts + over, b = k * parts + over, full = tiles * s / cus, late = tiles * s % cus;   // `late` units are busy for one more
         const int64_t t0 = full * a, t1 = late ? t0 + a : t0;
         // the first time by which the units that are free take all of the others
         int64_t lo = t1, hi = t1 + div_up(more, cus) * b + b;
@@ -672,6 +672,7 @@ static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k) 
         const int64_t cost = lo + s * over / 16;   // every run is added up once more at the end
         if (cost < least) { least = cost; best = s; }
     }
+    if (cost_of) *cost_of = least;
     return best;
 }
 
@@ -683,12 +684,29 @@ struct GradPlan {
     float *most, *coef, *gx;
     char *c, *x;
     LossParts parts;
+    // What a piece of p documents takes, in the units of pick_runs.
+    static double piece_cost(int64_t p, int64_t r, int64_t dim, int64_t parts, bool want_x) {
+        const int64_t tc = pick_tile(p, r), t = pick_tile(p, dim), more = div_up(p, t) * div_up(dim, t);
+        double cost = (double)(div_up(div_up(p, tc) * div_up(r, tc), 256) * (dim * parts + 512)) * tc * tc / 65536;
+        int64_t least = div_up(more, 256) * (r * parts + 512);
+        if (want_x) pick_runs(div_up(r, t) * div_up(dim, t), p, more, r, parts, &least);
+        return cost + (double)least * t * t / 65536 + 2 * 2048;   // two launches
+    }
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype, bool want_x) {
         LossWs ws{base};
         const int64_t r = std::max<int64_t>(rows, 1);
-        piece = std::max<int64_t>(AP_LOSS_PIECE_BYTES / (2 * r) / 256 * 256, 1024);
-        if (g_ap_debug.loss_piece) piece = up_to(g_ap_debug.loss_piece, 256);
-        piece = std::min(piece, up_to(n, 256));
+        const int64_t parts = dtype == AP_F32 ? 3 : 1;
+        piece = std::min(std::max<int64_t>(AP_LOSS_PIECE_BYTES / (2 * r) / 256 * 256, 1024), up_to(n, 256));
+        if (g_ap_debug.loss_piece) piece = std::min(up_to(g_ap_debug.loss_piece, 256), up_to(n, 256));
+        else if (piece < n) {   // several pieces: the length of which all of them take the least time
+            double least = 1e30;
+            int64_t best = piece;
+            for (int64_t p = piece; p >= piece / 2 && p >= 256; p -= up_to(piece / 32, 256)) {
+                const double t = (double)(n / p) * piece_cost(p, r, dim, parts, want_x) + (n % p ? piece_cost(up_to(n % p, 256), r, dim, parts, want_x) : 0);
+                if (t < least) { least = t; best = p; }
+            }
+            piece = best;
+        }
         ldc = piece * 2;
         // bf16 coefficients of few queries have a second part: a rounding of the label's alone would be seen in the result, and
         // where few are multiplied at once the second product costs little
@@ -699,14 +717,14 @@ struct GradPlan {
         tile = pick_tile(piece, dim);
         if (tile > 128 && r <= 128) tile = 128;
         if (tile > 64 && r <= 64) tile = 64;
-        runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r);
+        runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts);
         run_docs = (int32_t)up_to(div_up(piece, runs), 64);
         runs = (int32_t)div_up(piece, run_docs);
         most = ws.take<float>(1);
         coef = ws.take<float>(r);
         c = ws.take<char>(c_part * (dtype == AP_F32 || two ? 2 : 1));
         gx = want_x ? ws.take<float>(runs * r * dim) : nullptr;
-        if (dtype == AP_F32) parts.take(ws, r, n, dim);
+        if (dtype == AP_F32) this->parts.take(ws, r, n, dim);
         else x = ws.take<char>(r * dim * 2);
         return ws.bytes;
     }

@@ -63,12 +63,15 @@ __device__ __forceinline__ void ap_stream(const char *rows, int64_t ld, int64_t 
                 const int at = (s0 + i) * 64 + part;
                 a[i] = *reinterpret_cast<const ap_g_i32x4 *>(p + (at < row_bytes ? at : 0));
             }
+            __builtin_amdgcn_sched_barrier(0);   // all of them on their way before the first is waited for
 #pragma unroll
             for (int i = 0; i < AP_STREAM_AHEAD; i++) {
-                if (s0 + i >= steps) break;
-                if ((s0 + i) * 64 + part >= row_bytes) a[i] = ap_g_i32x4{0, 0, 0, 0};
+                const bool is = (s0 + i) * 64 + part < row_bytes;   // past the end of the row, and of what LDS holds: zeros
+                const int s = s0 + i < steps ? s0 + i : 0;
 #pragma unroll
-                for (int g = 0; g < NQ; g++) OP::mul(a[i], *reinterpret_cast<const ap_g_i32x4 *>(lds + (((s0 + i) * NQ + g) * 64 + lane) * 16), sums[g]);
+                for (int j = 0; j < 4; j++) a[i][j] = is ? a[i][j] : 0;
+#pragma unroll
+                for (int g = 0; g < NQ; g++) OP::mul(a[i], *reinterpret_cast<const ap_g_i32x4 *>(lds + ((s * NQ + g) * 64 + lane) * 16), sums[g]);
             }
         }
         typename OP::Acc acc[NQ];
