@@ -290,9 +290,10 @@ int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vocab, int32_
 int ap_embed_grad_bytes(int64_t n, int64_t vocab, int32_t dim, size_t *out);
 int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, int32_t dim, const ap_lists *lists, int64_t vocab,
                   float scale, void *grad_table, int32_t table_dtype, void *workspace, size_t bytes, void *stream);
+int ap_embed_grad_weights_bytes(int64_t n, int32_t dim, int32_t dtype, int32_t grad_dtype, size_t *out);
 int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t grad_dtype, const void *table, int64_t ld,
                           int32_t dtype, int64_t vocab, int32_t dim, const ap_lists *lists, float scale,
-                          float *grad_weights, void *stream);
+                          float *grad_weights, void *workspace, size_t bytes, void *stream);
 
 /* Rows in 8 bits: scale[r] = max |x[r]| / 127, q[r] = rint(x[r] / scale[r]) (f32, ties to even), zeros from column dim to
  * the next multiple of 16; ldq is at least that.  A row of zeros gets scale 0, one that holds an infinity or NaN zeros and

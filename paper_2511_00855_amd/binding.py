@@ -52,7 +52,7 @@ class _SearchParams(C.Structure):
 
 # Argument types of the calls that take plain numbers and addresses: p pointer, l int64, i int32, f float, z size_t.
 _KINDS = dict(p=C.c_void_p, l=C.c_int64, i=C.c_int32, f=C.c_float, z=C.c_size_t)
-_ARGTYPES = dict(ap_embed="plilipfpip", ap_embed_grad_bytes="llip", ap_embed_grad="pliiplfpipzp", ap_embed_grad_weights="pliplilipfpp",
+_ARGTYPES = dict(ap_embed="plilipfpip", ap_embed_grad_bytes="llip", ap_embed_grad="pliiplfpipzp", ap_embed_grad_weights_bytes="liiip", ap_embed_grad_weights="pliplilipfppzp",
                  ap_quantize_rows="plliiplpp", ap_scores_int8_bytes="liip", ap_scores_int8="plpliiplplplpzp",
                  ap_softmax_loss_bytes="lliip", ap_softmax_loss="pllplliifppppzp",
                  ap_softmax_loss_grad_bytes="lliiip", ap_softmax_loss_grad="pllplliifppppppzp")
@@ -610,7 +610,8 @@ def embed_grad_weights(grad_out: torch.Tensor, table: torch.Tensor, tokens: torc
     if l.rows != grad_out.shape[0]:
         raise ValueError(f"grad_out has {grad_out.shape[0]} rows for {l.rows} lists")
     out = torch.empty(l.n, dtype=torch.float32, device=table.device)
-    _call("ap_embed_grad_weights", table.device, pg, ldg, code_g, p, ld, code, table.shape[0], table.shape[1], C.byref(l), scale, out.data_ptr())
+    _call("ap_embed_grad_weights", table.device, pg, ldg, code_g, p, ld, code, table.shape[0], table.shape[1], C.byref(l), scale, out.data_ptr(),
+          bytes_args=(l.n, table.shape[1], code, code_g))
     return out
 
 

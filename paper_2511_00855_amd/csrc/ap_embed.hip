@@ -40,7 +40,7 @@ template <int OT, int N> __device__ __forceinline__ void put_row(void *row, int6
 struct ApEmbed {
     const char *table;             // or the gradient of the rows
     int64_t ld, vocab;             // ld in bytes
-    int32_t dim, lanes;            // lanes: threads a row, a power of two up to 64; each has 16 bytes at a time
+    int32_t dim;
     const int32_t *tokens;
     const float *weights;
     const int64_t *indptr;
@@ -49,25 +49,45 @@ struct ApEmbed {
     char *out;
 };
 
-#define AP_EMBED_AHEAD 8   // rows of the table that a thread has on their way
+// Columns go by slabs of 256 bytes: 16 lanes of 16.  Workgroups go round the eight XCDs, each with an L2 of 4 MB of its own; an XCD takes
+// one slab of everything before it takes the next, so that its L2 holds 256 bytes of 16,000 rows and not all columns of 2,000 (of Zipf(1.1) tokens,
+// seven of eight against three of four).  `units` workgroups make a slab; with a number of slabs that 8 does not divide, slabs are cut
+// into parts that go to several XCDs.
+struct ApSlabs { int32_t slabs, parts; int64_t units; };   // a part: units / parts workgroups, rounded up
+static ApSlabs slabs_of(int64_t bytes, int64_t units) {
+    const int32_t s = (int32_t)((bytes + 255) / 256);
+    int32_t parts = 8;
+    while (parts > 1 && s * (parts / 2) % 8 == 0) parts /= 2;
+    return ApSlabs{s, parts, units};
+}
+static int64_t slab_blocks(const ApSlabs &s) { return s.slabs * s.parts * ((s.units + s.parts - 1) / s.parts); }
+// The slab and the unit of a workgroup; false for one past the end.
+__device__ __forceinline__ bool slab_block(const ApSlabs &s, int32_t *slab, int64_t *unit) {
+    const int64_t each = (s.units + s.parts - 1) / s.parts;              // workgroups of a part
+    const int64_t x = blockIdx.x & 7, i = blockIdx.x >> 3, part = x * (s.slabs * s.parts / 8) + i / each;
+    *slab = (int32_t)(part / s.parts);
+    *unit = part % s.parts * each + i % each;
+    return *unit < s.units;
+}
 
-// `lanes` threads take one list and 16 bytes a thread of its columns at a time.  WAYS: as many waves share a list, each a run of its entries,
-// and the first adds up the sums.
-template <int DT, int OT, int WAYS>
-__global__ __launch_bounds__(256) void k_embed(ApEmbed p) {
+#define AP_EMBED_AHEAD 4   // loads of rows that a wave has on their way, four rows each
+
+// A wave takes a list and a slab, 64 entries at a time: each of its four groups of 16 lanes every fourth entry.  WAYS waves share a list.  Without
+// lists a wave takes 64 tokens and writes as many rows.
+template <int DT, int OT, int WAYS, bool LISTS>
+__global__ __launch_bounds__(256) void k_embed(ApEmbed p, ApSlabs s) {
     constexpr int N = ApRow16<DT>::N;
-    __shared__ float s_sum[WAYS > 1 ? 256 * N : 1];
-    const int groups = p.dim / N, slabs = (groups + p.lanes - 1) / p.lanes;   // of a row
-    const int per_wave = 64 / p.lanes, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t unit = WAYS > 1 ? (int64_t)blockIdx.x * per_wave + lane / p.lanes : ((int64_t)blockIdx.x * 4 + wave) * per_wave + lane / p.lanes;
-    const int64_t row = unit / slabs;
-    const int group = (int)(unit % slabs) * p.lanes + (lane & (p.lanes - 1));
-    const bool mine = row < p.rows && group < groups;
-    int64_t e = 0, end = 0;
-    if (mine) {
-        if (!p.indptr) { e = row; end = row + 1; }
-        else if (ap_row_ok(p.indptr, row, p.n)) { e = p.indptr[row]; end = p.indptr[row + 1]; }
-    }
+    __shared__ float s_sum[WAYS > 1 ? 4 * 16 * N : 1];
+    const int wave = ap_wave_id(), lane = threadIdx.x & 63, g = lane >> 4;
+    int32_t slab;
+    int64_t unit;
+    if (!slab_block(s, &slab, &unit)) return;
+    const int32_t col = (slab * 16 + (lane & 15)) * N;
+    const bool mine = col < p.dim;
+    const char *at = p.table + (mine ? col : 0) * (16 / N);
+    int64_t row = WAYS > 1 ? unit : unit * 4 + wave, e = 0, end = 0;
+    if (!LISTS) { e = row * 64; end = min(e + 64, p.n); }
+    else if (row < p.rows && ap_row_ok(p.indptr, row, p.n)) { e = p.indptr[row]; end = p.indptr[row + 1]; }
     if (WAYS > 1) {
         const int64_t each = (end - e + WAYS - 1) / WAYS, b = e + wave * each;
         end = min(end, b + each);
@@ -76,37 +96,58 @@ __global__ __launch_bounds__(256) void k_embed(ApEmbed p) {
     float sum[N];
 #pragma unroll
     for (int i = 0; i < N; i++) sum[i] = 0.f;
-    for (; e < end; e += AP_EMBED_AHEAD) {
-        uint4 v[AP_EMBED_AHEAD];
-        float w[AP_EMBED_AHEAD];
-#pragma unroll
-        for (int i = 0; i < AP_EMBED_AHEAD; i++) {
-            const int64_t at = e + i < end ? e + i : end - 1;
-            const int32_t t = p.tokens[at];
-            const bool used = e + i < end && t >= 0 && t < p.vocab;
-            w[i] = p.scale * (p.weights ? p.weights[at] : 1.f);
-            v[i] = make_uint4(0, 0, 0, 0);
-            if (used) v[i] = *reinterpret_cast<const uint4 *>(p.table + (int64_t)t * p.ld + group * 16);
-            else w[i] = 0.f;   // whatever weight a slot has that names no row
+    for (; e < end; e += 64) {
+        const int count = (int)min((int64_t)64, end - e);
+        int32_t tok = -1;
+        float w = 0.f;
+        if (lane < count) {
+            tok = p.tokens[e + lane];
+            if (tok >= p.vocab) tok = -1;
+            w = tok >= 0 ? p.scale * (p.weights ? p.weights[e + lane] : 1.f) : 0.f;   // whatever weight an unused slot has
         }
+        for (int i0 = 0; i0 < count; i0 += 4 * AP_EMBED_AHEAD) {
+            uint4 v[AP_EMBED_AHEAD];
+            float wi[AP_EMBED_AHEAD];
 #pragma unroll
-        for (int i = 0; i < AP_EMBED_AHEAD; i++) {
-            float x[N];
-            ApRow16<DT>::get(v[i], x);
+            for (int i = 0; i < AP_EMBED_AHEAD; i++) {
+                const int k = (i0 + i * 4 + g) & 63;
+                const int32_t t = __shfl(tok, k, 64);
+                wi[i] = __shfl(w, k, 64);
+                v[i] = make_uint4(0, 0, 0, 0);
+                if (t >= 0) v[i] = *reinterpret_cast<const uint4 *>(at + (int64_t)t * p.ld);
+            }
 #pragma unroll
-            for (int j = 0; j < N; j++) sum[j] = fmaf(w[i], x[j], sum[j]);
+            for (int i = 0; i < AP_EMBED_AHEAD; i++) {
+                float x[N];
+                ApRow16<DT>::get(v[i], x);
+                if (LISTS) {
+#pragma unroll
+                    for (int j = 0; j < N; j++) sum[j] = fmaf(wi[i], x[j], sum[j]);
+                } else if (mine && i0 + i * 4 + g < count) {
+#pragma unroll
+                    for (int j = 0; j < N; j++) x[j] *= wi[i];
+                    put_row<OT, N>(p.out + (e + i0 + i * 4 + g) * p.dim * (OT == AP_F32 ? 4 : 2), col, x);
+                }
+            }
         }
     }
-    if (WAYS > 1) {
+    if (!LISTS) return;
 #pragma unroll
-        for (int i = 0; i < N; i++) s_sum[i * 256 + threadIdx.x] = sum[i];
+    for (int j = 0; j < N; j++) {
+        sum[j] += __shfl_xor(sum[j], 16, 64);
+        sum[j] += __shfl_xor(sum[j], 32, 64);
+    }
+    if (WAYS > 1) {
+        if (g == 0)
+#pragma unroll
+            for (int j = 0; j < N; j++) s_sum[(wave * N + j) * 16 + lane] = sum[j];
         __syncthreads();
         if (wave) return;
         for (int k = 1; k < WAYS; k++)
 #pragma unroll
-            for (int i = 0; i < N; i++) sum[i] += s_sum[i * 256 + k * 64 + lane];
+            for (int j = 0; j < N; j++) sum[j] += s_sum[(k * N + j) * 16 + (lane & 15)];
     }
-    if (mine) put_row<OT, N>(p.out + row * p.dim * (OT == AP_F32 ? 4 : 2), group * N, sum);
+    if (mine && g == 0 && row < p.rows) put_row<OT, N>(p.out + row * p.dim * (OT == AP_F32 ? 4 : 2), col, sum);
 }
 
 // ------------------------------------------------------------------ gradient of the table
@@ -122,24 +163,54 @@ __device__ __forceinline__ int64_t row_of(const int64_t *indptr, int64_t rows, i
     return indptr[lo] <= e && e < indptr[lo + 1] ? lo : -1;
 }
 
-// Few entries: a wave takes an entry and a slab of its columns; if no earlier entry names the same token it adds up all that do, in order.
+#define AP_EMBED_FEW 4096   // entries that find their equals by reading the list
+// Few entries, one launch.  The first `owners` workgroups: a wave takes an entry and 1 KB of its columns; if no earlier entry names the same token it
+// adds up all that do, in order.  The others write zeros where no token points; which rows those are they see from a bitmap of the tokens (of
+// `bits` rows; 0: somebody else has written the zeros).
 template <int GT, int OT>
-__global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p) {
+__global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owners, int32_t bits) {
     constexpr int N = ApRow16<GT>::N;
-    const int groups = p.dim / N, slabs = (groups + 63) / 64, lane = threadIdx.x & 63;
+    extern __shared__ int32_t s_few[];
+    const int lane = threadIdx.x & 63;
+    if ((int32_t)blockIdx.x >= owners) {
+        uint32_t *map = reinterpret_cast<uint32_t *>(s_few);
+        for (int i = threadIdx.x; i < (bits + 31) / 32; i += 256) map[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.n; i += 256) {
+            const int32_t t = p.tokens[i];
+            if (t >= 0 && t < p.vocab) atomicOr(&map[t >> 5], 1u << (t & 31));
+        }
+        __syncthreads();
+        const int32_t groups = p.dim * (OT == AP_F32 ? 4 : 2) / 16, step = (gridDim.x - owners) * 256;
+        int32_t i = (blockIdx.x - owners) * 256 + threadIdx.x, row = i / groups, col = i - row * groups;
+        const int32_t rows = step / groups, cols = step - rows * groups;   // one step on
+        uint4 *to = reinterpret_cast<uint4 *>(p.out);
+        for (; row < p.vocab; ) {
+            if (!(map[row >> 5] >> (row & 31) & 1)) to[(int64_t)row * groups + col] = make_uint4(0, 0, 0, 0);
+            row += rows;
+            col += cols;
+            if (col >= groups) { col -= groups; row++; }
+        }
+        return;
+    }
+    for (int i = threadIdx.x; i < p.n; i += 256) s_few[i] = p.tokens[i];
+    __syncthreads();
+    const int groups = p.dim / N, slabs = (groups + 63) / 64;
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t e0 = unit / slabs;
+    const int e0 = (int)(unit / slabs);
     if (e0 >= p.n) return;
-    const int32_t t = p.tokens[e0];
+    const int32_t t = s_few[e0];
     if (t < 0 || t >= p.vocab) return;
-    for (int64_t e = 0; e < e0; e += 64)
-        if (__any(e + lane < e0 && p.tokens[e + lane] == t)) return;
+    bool earlier = false;
+    for (int e = lane; e < e0; e += 64) earlier |= s_few[e] == t;
+    if (__any(earlier)) return;
     const int group = (int)(unit % slabs) * 64 + lane;
     float sum[N];
 #pragma unroll
     for (int i = 0; i < N; i++) sum[i] = 0.f;
-    for (int64_t e = e0; e < p.n; e += 64) {
-        const bool same = e + lane < p.n && p.tokens[e + lane] == t;
+    for (int e = e0; e < p.n; e += 64) {
+        const bool same = e + lane < p.n && s_few[e + lane] == t;
+        if (!__any(same)) continue;
         int64_t row = -1;
         float w = 0.f;
         if (same) { row = row_of(p.indptr, p.rows, e + lane); w = p.scale * (p.weights ? p.weights[e + lane] : 1.f); }
@@ -158,8 +229,8 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p) {
     if (group < groups) put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), group * N, sum);
 }
 
-// Stable radix sort of the entries by token: 4,096 entries a block, up to 9 bits a pass.  What names no row of the table sorts last.
-#define AP_SORT_ITEMS 4096
+// Stable radix sort of the entries by token: 2,048 entries a block, up to 9 bits a pass.  What names no row of the table sorts last.
+#define AP_SORT_ITEMS 2048
 #define AP_SORT_BINS 512
 __device__ __forceinline__ uint32_t sort_key(const int32_t *tokens, int64_t vocab, int64_t i) { const int32_t t = tokens[i]; return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab; }
 
@@ -177,43 +248,49 @@ __global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ 
     __syncthreads();
     for (int b = threadIdx.x; b < 1 << bits; b += 256) hist[b * blocks + blockIdx.x] = s_cnt[b];
 }
-__global__ __launch_bounds__(1024) void k_sort_scan(uint32_t *__restrict__ h, int64_t count) {   // exclusive sums, by one block
-    __shared__ uint32_t s_wave[16];
-    uint32_t before = 0;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int64_t i0 = 0; i0 < count; i0 += 4096) {
-        const int64_t at = i0 + threadIdx.x * 4;
-        uint32_t v[4], own = 0;
-#pragma unroll
-        for (int j = 0; j < 4; j++) { v[j] = at + j < count ? h[at + j] : 0; own += v[j]; }
+// A wave makes the counts of a bin into sums over the blocks before, and leaves the bin's total behind them.
+__global__ __launch_bounds__(256) void k_sort_scan(uint32_t *__restrict__ hist, int64_t blocks, int bins, uint32_t *__restrict__ totals) {
+    const int lane = threadIdx.x & 63, bin = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (bin >= bins) return;
+    uint32_t *h = hist + bin * blocks, before = 0;
+    for (int64_t i = 0; i < blocks; i += 64) {
+        const uint32_t own = i + lane < blocks ? h[i + lane] : 0;
         uint32_t sum = own;
         for (int o = 1; o < 64; o <<= 1) { const uint32_t t = __shfl_up(sum, o, 64); if (lane >= o) sum += t; }
-        if (lane == 63) s_wave[wave] = sum;
-        __syncthreads();
-        uint32_t base = before, all = 0;
-        for (int w = 0; w < 16; w++) { if (w < wave) base += s_wave[w]; all += s_wave[w]; }
-        base += sum - own;
-#pragma unroll
-        for (int j = 0; j < 4; j++) { if (at + j < count) h[at + j] = base; base += v[j]; }
-        before += all;
-        __syncthreads();
+        if (i + lane < blocks) h[i + lane] = before + sum - own;
+        before += __shfl(sum, 63, 64);
     }
+    if (lane == 0) totals[bin] = before;
+}
+// The list of every entry.
+__global__ __launch_bounds__(256) void k_sort_rows(ApEmbed p, int32_t *__restrict__ row) {
+    for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < p.n; e += (int64_t)gridDim.x * 256) row[e] = (int32_t)row_of(p.indptr, p.rows, e);
 }
 // The last pass also brings along what the sums need of an entry: its row (-1: none) and its weight.
 __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t *__restrict__ keys, const int32_t *__restrict__ entries, int shift, int bits, const uint32_t *__restrict__ hist,
-                                                      int64_t blocks, uint32_t *__restrict__ keys_out, int32_t *__restrict__ entries_out, int last, int32_t *__restrict__ row_out,
-                                                      float *__restrict__ w_out) {
-    __shared__ uint32_t s_at[4][AP_SORT_BINS];
+                                                      int64_t blocks, const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys_out, int32_t *__restrict__ entries_out, int last,
+                                                      const int32_t *__restrict__ row_in, int32_t *__restrict__ row_out, float *__restrict__ w_out) {
+    __shared__ uint32_t s_at[4][AP_SORT_BINS], s_first[AP_SORT_BINS], s_wave[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t mask = (1u << bits) - 1;
     for (int b = threadIdx.x; b < 4 * AP_SORT_BINS; b += 256) (&s_at[0][0])[b] = 0;
+    {   // where the bins begin: two of them a thread
+        const uint32_t b = threadIdx.x * 2, x = b <= mask ? totals[b] : 0, y = b + 1 <= mask ? totals[b + 1] : 0;
+        uint32_t sum = x + y;
+        for (int o = 1; o < 64; o <<= 1) { const uint32_t v = __shfl_up(sum, o, 64); if (lane >= o) sum += v; }
+        if (lane == 63) s_wave[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < wave; w++) sum += s_wave[w];
+        s_first[b] = sum - x - y;
+        s_first[b + 1] = sum - y;
+    }
     __syncthreads();
     const int64_t i0 = (int64_t)blockIdx.x * AP_SORT_ITEMS + wave * (AP_SORT_ITEMS / 4);   // a wave's entries lie together
     for (int i = lane; i < AP_SORT_ITEMS / 4; i += 64)
         if (i0 + i < p.n) atomicAdd(&s_at[wave][((keys ? keys[i0 + i] : sort_key(p.tokens, p.vocab, i0 + i)) >> shift) & mask], 1u);
     __syncthreads();
     for (uint32_t b = threadIdx.x; b <= mask; b += 256) {
-        uint32_t at = hist[b * blocks + blockIdx.x];
+        uint32_t at = s_first[b] + hist[b * blocks + blockIdx.x];
 #pragma unroll
         for (int w = 0; w < 4; w++) { const uint32_t c = s_at[w][b]; s_at[w][b] = at; at += c; }
     }
@@ -233,58 +310,62 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t 
             const int64_t e = entries ? entries[i0 + i + lane] : i0 + i + lane;
             keys_out[at] = k;
             if (!last) entries_out[at] = (int32_t)e;
-            else { row_out[at] = (int32_t)row_of(p.indptr, p.rows, e); w_out[at] = p.scale * (p.weights ? p.weights[e] : 1.f); }
+            else { row_out[at] = row_in ? row_in[e] : (int32_t)e; w_out[at] = p.scale * (p.weights ? p.weights[e] : 1.f); }
         }
     }
 }
 
-// A run of `run` sorted entries, a slab of 16 bytes a lane.  Tokens whose entries all lie in the run are written; the sum of a token that began
+// 16 lanes take a run of `run` sorted entries and a slab.  Tokens whose entries all lie in the run are written; the sum of a token that began
 // in an earlier run goes to carry[run][0], that of one that goes on in the next to carry[run][1].
 struct ApRuns { const uint32_t *keys; const int32_t *rows; const float *w; float *carry; int32_t run; };
 template <int GT, int OT>
-__global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s) {
+__global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, ApSlabs sl) {
     constexpr int N = ApRow16<GT>::N;
-    const int groups = p.dim / N, slabs = (groups + 63) / 64, lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), run = unit / slabs;
+    int32_t slab;
+    int64_t unit;
+    if (!slab_block(sl, &slab, &unit)) return;
+    const int l16 = threadIdx.x & 15;
+    const int64_t run = unit * 16 + (threadIdx.x >> 4);
     const int64_t b = run * s.run, end = min(b + s.run, p.n);
     if (b >= p.n || s.keys[b] >= p.vocab) return;
-    const int group = (int)(unit % slabs) * 64 + lane;
-    const bool mine = group < groups;
+    const int32_t col = (slab * 16 + l16) * N;
+    const bool mine = col < p.dim;
+    const char *at = p.table + (mine ? col : 0) * (16 / N);
     float sum[N];
 #pragma unroll
     for (int i = 0; i < N; i++) sum[i] = 0.f;
     bool begun = b > 0 && s.keys[b - 1] == s.keys[b];   // the present token began in an earlier run
-    for (int64_t e = b; e < end; e += 64) {
-        const bool is = e + lane < end;
-        const uint32_t key = is ? s.keys[e + lane] : 0xffffffffu;
-        const uint32_t next = e + lane + 1 < p.n ? s.keys[min(e + lane + 1, p.n - 1)] : 0xffffffffu;
-        const int32_t row = is ? s.rows[e + lane] : -1;
-        const float w = is ? s.w[e + lane] : 0.f;
-        const int count = (int)min((int64_t)64, end - e);
-        for (int k0 = 0; k0 < count; k0 += 8) {
+    for (int64_t e = b; e < end; e += 16) {
+        const bool is = e + l16 < end;
+        const uint32_t key = is ? s.keys[e + l16] : 0xffffffffu;
+        const uint32_t next = e + l16 + 1 < p.n ? s.keys[e + l16 + 1] : 0xffffffffu;
+        const int32_t row = is && key < p.vocab ? s.rows[e + l16] : -1;   // -1 also for an entry of no list
+        const float w = is ? s.w[e + l16] : 0.f;
+        // 1: the token's sum ends here, 2: it goes on in the next run
+        const int32_t what = is && key < p.vocab ? (next != key ? 1 : e + l16 + 1 == end ? 2 : 0) : 0;
+#pragma unroll
+        for (int k0 = 0; k0 < 16; k0 += 8) {
             uint4 v[8];
 #pragma unroll
             for (int k = 0; k < 8; k++) {
-                const int32_t r = __builtin_amdgcn_readlane(row, k0 + k);   // -1 past the end of the run
+                const int32_t r = __shfl(row, k0 + k, 16);
                 v[k] = make_uint4(0, 0, 0, 0);
-                if (r >= 0 && mine) v[k] = *reinterpret_cast<const uint4 *>(p.table + r * p.ld + group * 16);
+                if (r >= 0) v[k] = *reinterpret_cast<const uint4 *>(at + (int64_t)r * p.ld);
             }
 #pragma unroll
             for (int k = 0; k < 8; k++) {
-                const uint32_t t = __builtin_amdgcn_readlane(key, k0 + k);
-                if (t >= p.vocab) break;   // the end, or what names no row
-                const float wk = __builtin_amdgcn_readlane(row, k0 + k) >= 0 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k0 + k)) : 0.f;
+                const float wk = __shfl(row, k0 + k, 16) >= 0 ? __shfl(w, k0 + k, 16) : 0.f;
+                const int32_t end_k = __shfl(what, k0 + k, 16);
+                const uint32_t t = __shfl(key, k0 + k, 16);
                 float x[N];
                 ApRow16<GT>::get(v[k], x);
 #pragma unroll
                 for (int j = 0; j < N; j++) sum[j] = fmaf(wk, x[j], sum[j]);
-                const bool ends = (uint32_t)__builtin_amdgcn_readlane(next, k0 + k) != t;
-                const bool leaves = !ends && e + k0 + k + 1 == end;
-                if (!ends && !leaves) continue;
+                if (!end_k) continue;
                 if (mine) {
-                    if (begun) put_row<AP_F32, N>(s.carry + run * 2 * p.dim, group * N, sum);
-                    else if (leaves) put_row<AP_F32, N>(s.carry + (run * 2 + 1) * p.dim, group * N, sum);
-                    else put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), group * N, sum);
+                    if (begun) put_row<AP_F32, N>(s.carry + run * 2 * p.dim, col, sum);
+                    else if (end_k == 2) put_row<AP_F32, N>(s.carry + (run * 2 + 1) * p.dim, col, sum);
+                    else put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), col, sum);
                 }
 #pragma unroll
                 for (int j = 0; j < N; j++) sum[j] = 0.f;
@@ -329,43 +410,62 @@ __global__ __launch_bounds__(1024) void k_embed_grad_join(ApEmbed p, ApRuns s, i
 }
 
 // ------------------------------------------------------------------ gradient of the weights
-// A wave takes 8 entries in a row.  g: the gradient of the rows.
+// 16 lanes take an entry and a slab of it; a wave 16 entries in a row.  A slab's part goes to out[slab][entry].
 template <int DT, int GT>
-__global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, const char *__restrict__ g, int64_t ldg, float *__restrict__ out) {
-    const int lane = threadIdx.x & 63;
-    const int64_t e0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 8;
+__global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s, const int32_t *__restrict__ rows /* of every entry; NULL: looked up */, const char *__restrict__ g, int64_t ldg,
+                                                            float *__restrict__ out) {
+    // 16 bytes of the wider type: four or eight columns a lane
+    constexpr int N = DT == AP_BF16 && GT == AP_BF16 ? 8 : 4;
+    int32_t slab;
+    int64_t unit;
+    if (!slab_block(s, &slab, &unit)) return;
+    const int lane = threadIdx.x & 63, l16 = lane & 15;
+    const int64_t e0 = (unit * 4 + (threadIdx.x >> 6)) * 16;
     if (e0 >= p.n) return;
-    const int64_t e = e0 + (lane & 7);
-    int64_t row = -1;
-    int32_t tok = -1;
-    if (e < p.n) { tok = p.tokens[e]; row = tok >= 0 && tok < p.vocab ? row_of(p.indptr, p.rows, e) : -1; }
-    float sum[8];
-    const char *a8[8], *b8[8];   // the rows of each entry; NULL: it has none
-#pragma unroll
-    for (int k = 0; k < 8; k++) {
-        const int32_t r = __builtin_amdgcn_readlane((int32_t)row, k), t = __builtin_amdgcn_readlane(tok, k);
-        sum[k] = 0.f;
-        a8[k] = r < 0 ? nullptr : p.table + (int64_t)t * p.ld;
-        b8[k] = r < 0 ? nullptr : g + r * ldg;
+    int32_t row = -1, tok = -1;
+    if (e0 + l16 < p.n) {
+        tok = p.tokens[e0 + l16];
+        if (tok >= p.vocab) tok = -1;
+        if (tok >= 0) row = rows ? rows[e0 + l16] : (int32_t)row_of(p.indptr, p.rows, e0 + l16);
     }
-    for (int c = lane * 4; c < p.dim; c += 256) {
+    const int32_t col = (slab * 16 + l16) * N;
+    const bool mine = col < p.dim;
+    const char *a = p.table + (mine ? col : 0) * (DT == AP_F32 ? 4 : 2), *b = g + (mine ? col : 0) * (GT == AP_F32 ? 4 : 2);
+    float sum[4];
+    uint4 x[4], y[4];
+    bool used[4];
 #pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const char *a = a8[k], *b = b8[k];
-            if (!a) continue;
-            float x[4], y[4];
-            if (DT == AP_F32) { const float4 v = *reinterpret_cast<const float4 *>(a + c * 4); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
-            else { const uint2 v = *reinterpret_cast<const uint2 *>(a + c * 2); x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u); x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u); }
-            if (GT == AP_F32) { const float4 v = *reinterpret_cast<const float4 *>(b + c * 4); y[0] = v.x; y[1] = v.y; y[2] = v.z; y[3] = v.w; }
-            else { const uint2 v = *reinterpret_cast<const uint2 *>(b + c * 2); y[0] = __uint_as_float(v.x << 16); y[1] = __uint_as_float(v.x & 0xffff0000u); y[2] = __uint_as_float(v.y << 16); y[3] = __uint_as_float(v.y & 0xffff0000u); }
-#pragma unroll
-            for (int j = 0; j < 4; j++) sum[k] = fmaf(x[j], y[j], sum[k]);
-        }
+    for (int i = 0; i < 4; i++) {   // entry 4 i + lane / 16
+        const int32_t t = __shfl(tok, i * 4 + (lane >> 4), 64), r = __shfl(row, i * 4 + (lane >> 4), 64);
+        used[i] = r >= 0 && mine;
+        x[i] = y[i] = make_uint4(0, 0, 0, 0);
+        if (!used[i]) continue;
+        const char *pa = a + (int64_t)t * p.ld, *pb = b + (int64_t)r * ldg;
+        if (DT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pa); x[i].x = v.x; x[i].y = v.y; } else x[i] = *reinterpret_cast<const uint4 *>(pa);
+        if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pb); y[i].x = v.x; y[i].y = v.y; } else y[i] = *reinterpret_cast<const uint4 *>(pb);
     }
 #pragma unroll
-    for (int k = 0; k < 8; k++) {
-        const float v = ap_wave_sum(sum[k]) * p.scale;
-        if (lane == k && e < p.n) out[e] = v;
+    for (int i = 0; i < 4; i++) {
+        float u[8], v[8];
+        ApRow16<DT>::get(x[i], u);
+        ApRow16<GT>::get(y[i], v);
+        sum[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; j++) sum[i] = fmaf(u[j], v[j], sum[i]);
+        sum[i] += ap_dpp<0xB1>(sum[i]);
+        sum[i] += ap_dpp<0x4E>(sum[i]);
+        sum[i] += ap_dpp<0x141>(sum[i]);
+        sum[i] += ap_dpp<0x140>(sum[i]);
+        const int64_t e = e0 + i * 4 + (lane >> 4);
+        if (l16 == 0 && e < p.n) out[slab * p.n + e] = sum[i] * p.scale;
+    }
+}
+__global__ __launch_bounds__(256) void k_embed_grad_weights_sum(const float *__restrict__ parts, int64_t n, int32_t slabs, float *__restrict__ out) {
+    for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
+        float v = 0.f;
+#pragma unroll 4
+        for (int32_t s = 0; s < slabs; s++) v += parts[s * n + e];
+        out[e] = v;
     }
 }
 
@@ -389,7 +489,7 @@ static int check_lists(const ap_lists *l, int64_t vocab) {
     return AP_OK;
 }
 static ApEmbed args_of(const void *table, int64_t ld, int32_t dtype, int64_t vocab, int32_t dim, const ap_lists *l, float scale, void *out) {
-    return ApEmbed{static_cast<const char *>(table), ld * (dtype == AP_BF16 ? 2 : 4), vocab, dim, 64, l->tokens, l->weights, l->indptr, l->n, l->rows, scale, static_cast<char *>(out)};
+    return ApEmbed{static_cast<const char *>(table), ld * (dtype == AP_BF16 ? 2 : 4), vocab, dim, l->tokens, l->weights, l->indptr, l->n, l->rows, scale, static_cast<char *>(out)};
 }
 #define AP_TYPES(a, b, CALL)                                              \
     do {                                                                  \
@@ -406,31 +506,29 @@ extern "C" int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vo
     if (lists->rows == 0) return AP_OK;
     AP_TRY(check_matrix("out", out, dim, dim, out_dtype));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, out);
-    const int groups = dim / (dtype == AP_BF16 ? 8 : 4);
-    while (p.lanes / 2 >= groups) p.lanes /= 2;
-    const int64_t units = lists->rows * div_up(groups, p.lanes), waves = div_up(units, 64 / p.lanes);
+    const ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, out);
+    const int64_t bytes = (int64_t)dim * (dtype == AP_BF16 ? 2 : 4);
     // few waves with long lists: four share a list
-    const bool share = waves < 4096 && lists->n / lists->rows >= 16;
-    const int64_t blocks = share ? waves : div_up(waves, 4);
-    AP_REQUIRE(blocks < (1ll << 23), "too many rows");
-#define AP_EMBED(A, B)                                                                                                   \
-    do {                                                                                                                 \
-        if (share) hipLaunchKernelGGL((k_embed<A, B, 4>), dim3((unsigned)blocks), dim3(256), 0, st, p);                  \
-        else hipLaunchKernelGGL((k_embed<A, B, 1>), dim3((unsigned)blocks), dim3(256), 0, st, p);                        \
+    const bool share = lists->indptr && lists->rows * div_up(bytes, 256) < 8192 && lists->n / lists->rows >= 64;
+    const ApSlabs s = slabs_of(bytes, !lists->indptr ? div_up(lists->n, 256) : share ? lists->rows : div_up(lists->rows, 4));
+    AP_REQUIRE(slab_blocks(s) < (1ll << 23), "too many rows");
+    const dim3 grid((unsigned)slab_blocks(s));
+#define AP_EMBED(A, B)                                                                                    \
+    do {                                                                                                  \
+        if (!lists->indptr) hipLaunchKernelGGL((k_embed<A, B, 1, false>), grid, dim3(256), 0, st, p, s);  \
+        else if (share) hipLaunchKernelGGL((k_embed<A, B, 4, true>), grid, dim3(256), 0, st, p, s);       \
+        else hipLaunchKernelGGL((k_embed<A, B, 1, true>), grid, dim3(256), 0, st, p, s);                  \
     } while (0)
     AP_TYPES(dtype, out_dtype, AP_EMBED);
 #undef AP_EMBED
     return AP_OK;
 }
 
-#define AP_EMBED_FEW 4096   // entries that find their equals by reading the list
-
 struct GradWs {
     int64_t blocks, runs;
     int32_t run, passes, bits;
-    uint32_t *keys[2], *hist;
-    int32_t *entries[2], *rows;
+    uint32_t *keys[2], *hist, *totals;
+    int32_t *entries[2], *rows, *rows_in;
     float *w, *carry;
     size_t lay(char *base, int64_t n, int64_t vocab, int32_t dim) {
         size_t at = 0;
@@ -440,12 +538,14 @@ struct GradWs {
         passes = (int32_t)div_up(all, 9);
         bits = (int32_t)div_up(all, passes);
         blocks = div_up(n, AP_SORT_ITEMS);
-        run = 64;
+        run = 64;   // as long as they fill the compute units: every run leaves two rows of sums behind
         while (run < 256 && n / run > 8192) run *= 2;
         runs = div_up(n, run);
         for (int i = 0; i < 2; i++) { keys[i] = (uint32_t *)take(n); entries[i] = (int32_t *)take(n); }
         hist = (uint32_t *)take(blocks << bits);
+        totals = (uint32_t *)take(1ll << bits);
         rows = (int32_t *)take(n);
+        rows_in = (int32_t *)take(n);
         w = (float *)take(n);
         carry = (float *)take(runs * 2 * dim);
         return at;
@@ -471,31 +571,36 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     const size_t need = embed_few(lists->n) ? 0 : ws.lay(static_cast<char *>(workspace), lists->n, vocab, dim);
     AP_REQUIRE(bytes >= need && (workspace || need == 0), "workspace of %zu bytes, %zu are needed", bytes, need);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t words = vocab * dim / (table_dtype == AP_BF16 ? 8 : 4);
-    hipLaunchKernelGGL(k_embed_zero, dim3((unsigned)std::min<int64_t>(div_up(words, 256), 8192)), dim3(256), 0, st, static_cast<uint4 *>(grad_table), words);
-    AP_CHECK_HIP(hipGetLastError());
-    if (lists->n == 0 || lists->rows == 0) return AP_OK;
     ApEmbed p = args_of(grad_out, ld, dtype, vocab, dim, lists, scale, grad_table);
-    const int64_t slabs = div_up(dim / (dtype == AP_BF16 ? 8 : 4), 64);
-    if (embed_few(lists->n)) {
-        const dim3 grid((unsigned)div_up(lists->n * slabs, 4));
-#define AP_FEW(A, B) hipLaunchKernelGGL((k_embed_grad_few<A, B>), grid, dim3(256), 0, st, p)
+    const int64_t words = vocab * dim / (table_dtype == AP_BF16 ? 8 : 4);
+    const bool any = lists->n > 0 && lists->rows > 0, few = embed_few(lists->n), one = any && few && vocab <= (1 << 18);   // bits of a bitmap in LDS
+    if (!one) hipLaunchKernelGGL(k_embed_zero, dim3((unsigned)std::min<int64_t>(div_up(words, 256), 8192)), dim3(256), 0, st, static_cast<uint4 *>(grad_table), words);
+    AP_CHECK_HIP(hipGetLastError());
+    if (!any) return AP_OK;
+    if (few) {
+        const int32_t owners = (int32_t)div_up(lists->n * div_up(dim / (dtype == AP_BF16 ? 8 : 4), 64), 4), bits = one ? (int32_t)vocab : 0;
+        const size_t lds = std::max<size_t>((size_t)lists->n * 4, (size_t)(bits + 31) / 32 * 4);
+        const dim3 grid((unsigned)(owners + (one ? std::min<int64_t>(div_up(words, 1024), 1024) : 0)));
+#define AP_FEW(A, B) hipLaunchKernelGGL((k_embed_grad_few<A, B>), grid, dim3(256), lds, st, p, owners, bits)
         AP_TYPES(dtype, table_dtype, AP_FEW);
 #undef AP_FEW
         return AP_OK;
     }
+    if (lists->indptr) hipLaunchKernelGGL(k_sort_rows, dim3((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192)), dim3(256), 0, st, p, ws.rows_in);
     for (int i = 0; i < ws.passes; i++) {
         const uint32_t *keys = i ? ws.keys[(i - 1) & 1] : nullptr;
         const int32_t *entries = i ? ws.entries[(i - 1) & 1] : nullptr;
         hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, keys, lists->n, i * ws.bits, ws.bits, ws.hist, ws.blocks);
-        hipLaunchKernelGGL(k_sort_scan, dim3(1), dim3(1024), 0, st, ws.hist, ws.blocks << ws.bits);
-        hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, keys, entries, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.keys[i & 1], ws.entries[i & 1],
-                           i + 1 == ws.passes, ws.rows, ws.w);
+        hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)div_up(1 << ws.bits, 4)), dim3(256), 0, st, ws.hist, ws.blocks, 1 << ws.bits, ws.totals);
+        hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, keys, entries, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.totals, ws.keys[i & 1],
+                           ws.entries[i & 1], i + 1 == ws.passes, lists->indptr ? ws.rows_in : nullptr, ws.rows, ws.w);
         AP_CHECK_HIP(hipGetLastError());
     }
     const ApRuns s{ws.keys[(ws.passes - 1) & 1], ws.rows, ws.w, ws.carry, ws.run};
-    const dim3 grid((unsigned)div_up(ws.runs * slabs, 4)), joins((unsigned)ws.runs, (unsigned)std::max<int64_t>(1, std::min<int64_t>(div_up(dim, 256), (1ll << 21) / ws.runs)));   // below 2^31 threads
-#define AP_RUNS(A, B) hipLaunchKernelGGL((k_embed_grad_runs<A, B>), grid, dim3(256), 0, st, p, s)
+    const ApSlabs sl = slabs_of((int64_t)dim * (dtype == AP_BF16 ? 2 : 4), div_up(ws.runs, 16));
+    AP_REQUIRE(slab_blocks(sl) < (1ll << 23), "too many entries");
+    const dim3 grid((unsigned)slab_blocks(sl)), joins((unsigned)ws.runs, (unsigned)std::max<int64_t>(1, std::min<int64_t>(div_up(dim, 256), (1ll << 21) / ws.runs)));   // below 2^31 threads
+#define AP_RUNS(A, B) hipLaunchKernelGGL((k_embed_grad_runs<A, B>), grid, dim3(256), 0, st, p, s, sl)
     AP_TYPES(dtype, table_dtype, AP_RUNS);
 #undef AP_RUNS
     if (table_dtype == AP_F32) hipLaunchKernelGGL((k_embed_grad_join<AP_F32>), joins, dim3(1024), 0, st, p, s, ws.runs);
@@ -504,21 +609,50 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     return AP_OK;
 }
 
+// The workspace of the weights' gradient: the parts of each slab, and for many entries of lists the list of each.
+static void weights_layout(int64_t n, int32_t dim, int32_t dtype, int32_t grad_dtype, int32_t *slabs, size_t *parts, size_t *rows) {
+    *slabs = (int32_t)div_up(dim, dtype == AP_BF16 && grad_dtype == AP_BF16 ? 128 : 64);
+    *parts = *slabs > 1 ? (size_t)div_up(n * *slabs * 4, 256) * 256 : 0;
+    *rows = n > AP_EMBED_FEW ? (size_t)n * 4 : 0;
+}
+
+extern "C" int ap_embed_grad_weights_bytes(int64_t n, int32_t dim, int32_t dtype, int32_t grad_dtype, size_t *out) {
+    AP_REQUIRE(out != nullptr, "out is NULL");
+    AP_REQUIRE(n >= 0 && n < (1ll << 28) && dim >= 1 && dim <= 8192, "n or dim is out of range");
+    int32_t slabs;
+    size_t parts, rows;
+    weights_layout(n, dim, dtype, grad_dtype, &slabs, &parts, &rows);
+    *out = parts + rows;
+    return AP_OK;
+}
+
 extern "C" int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t grad_dtype, const void *table, int64_t ld, int32_t dtype, int64_t vocab, int32_t dim, const ap_lists *lists,
-                                     float scale, float *grad_weights, void *stream) {
+                                     float scale, float *grad_weights, void *workspace, size_t bytes, void *stream) {
     AP_TRY(check_lists(lists, vocab));
     if (lists->n == 0) return AP_OK;
     AP_TRY(check_matrix("table", table, ld, dim, dtype));
     if (lists->rows) AP_TRY(check_matrix("grad_out", grad_out, ldg, dim, grad_dtype));
     AP_REQUIRE(grad_weights != nullptr, "grad_weights is NULL");
+    int32_t slabs;
+    size_t part_bytes, row_bytes;
+    weights_layout(lists->n, dim, dtype, grad_dtype, &slabs, &part_bytes, &row_bytes);
+    const size_t need = part_bytes + row_bytes;
+    AP_REQUIRE(bytes >= need && (workspace || need == 0), "workspace of %zu bytes, %zu are needed", bytes, need);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (lists->rows == 0) return ap_fill_u32(grad_weights, (size_t)lists->n, 0, st);
     const ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, nullptr);
     const char *g = static_cast<const char *>(grad_out);
     const int64_t ldb = ldg * (grad_dtype == AP_BF16 ? 2 : 4);
-    if (lists->rows == 0) return ap_fill_u32(grad_weights, (size_t)lists->n, 0, st);
-    const dim3 grid((unsigned)div_up(lists->n, 32));
-#define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(256), 0, st, p, g, ldb, grad_weights)
+    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, 64));
+    AP_REQUIRE(slab_blocks(s) < (1ll << 23), "too many entries");
+    const dim3 grid((unsigned)slab_blocks(s)), flat((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192));
+    float *parts = slabs > 1 ? static_cast<float *>(workspace) : grad_weights;
+    int32_t *rows = lists->indptr && row_bytes ? reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + part_bytes) : nullptr;
+    if (rows) hipLaunchKernelGGL(k_sort_rows, flat, dim3(256), 0, st, p, rows);
+#define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(256), 0, st, p, s, rows, g, ldb, parts)
     AP_TYPES(dtype, grad_dtype, AP_WEIGHTS);
 #undef AP_WEIGHTS
+    if (slabs > 1) hipLaunchKernelGGL(k_embed_grad_weights_sum, flat, dim3(256), 0, st, parts, lists->n, slabs, grad_weights);
+    AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }
