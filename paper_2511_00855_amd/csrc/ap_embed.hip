@@ -8,6 +8,7 @@
 // so that a token's entries stay in their order) and cut into runs of one length, whatever the tokens' frequencies; a token
 // whose entries lie in several runs gets the runs' sums added in their order.  No sum depends on which wave came first.
 #include <algorithm>
+#include <type_traits>
 #include "ap_common.hpp"
 
 template <int DT> struct ApRow16;   // 16 bytes of a row as f32
@@ -34,6 +35,17 @@ template <int OT, int N> __device__ __forceinline__ void put_row(void *row, int6
         __bf16 *p = static_cast<__bf16 *>(row) + col;
 #pragma unroll
         for (int i = 0; i < N; i += 4) *reinterpret_cast<b4 *>(p + i) = b4{(__bf16)v[i], (__bf16)v[i + 1], (__bf16)v[i + 2], (__bf16)v[i + 3]};
+    }
+}
+
+// Lane K's value in every row of 16 lanes.
+template <int K> __device__ __forceinline__ int32_t row_bcast(int32_t v) { return __builtin_amdgcn_update_dpp(0, v, 0x150 + K, 0xf, 0xf, true); }
+template <int K> __device__ __forceinline__ float row_bcast(float v) { return __int_as_float(row_bcast<K>(__float_as_int(v))); }
+// f(0), f(1), .. f(N - 1) with constants
+template <int N, class F> __device__ __forceinline__ void for_each_const(F f) {
+    if constexpr (N > 0) {
+        for_each_const<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
     }
 }
 
@@ -97,39 +109,38 @@ __global__ __launch_bounds__(256) void k_embed(ApEmbed p, ApSlabs s) {
 #pragma unroll
     for (int i = 0; i < N; i++) sum[i] = 0.f;
     for (; e < end; e += 64) {
-        const int count = (int)min((int64_t)64, end - e);
+        const int count = (int)min((int64_t)64, end - e), own = (lane & 15) * 4 + g;   // lane i of a group brings the group's entry i: 4 i + g
         int32_t tok = -1;
         float w = 0.f;
-        if (lane < count) {
-            tok = p.tokens[e + lane];
+        if (own < count) {
+            tok = p.tokens[e + own];
             if (tok >= p.vocab) tok = -1;
-            w = tok >= 0 ? p.scale * (p.weights ? p.weights[e + lane] : 1.f) : 0.f;   // whatever weight an unused slot has
+            w = tok >= 0 ? p.scale * (p.weights ? p.weights[e + own] : 1.f) : 0.f;   // whatever weight an unused slot has
         }
-        for (int i0 = 0; i0 < count; i0 += 4 * AP_EMBED_AHEAD) {
+        for_each_const<16 / AP_EMBED_AHEAD>([&](auto i0) {
+            constexpr int I0 = decltype(i0)::value * AP_EMBED_AHEAD;
+            if (I0 * 4 >= count) return;
             uint4 v[AP_EMBED_AHEAD];
             float wi[AP_EMBED_AHEAD];
-#pragma unroll
-            for (int i = 0; i < AP_EMBED_AHEAD; i++) {
-                const int k = (i0 + i * 4 + g) & 63;
-                const int32_t t = __shfl(tok, k, 64);
-                wi[i] = __shfl(w, k, 64);
+            for_each_const<AP_EMBED_AHEAD>([&](auto i) {
+                const int32_t t = row_bcast<I0 + i>(tok);
+                wi[i] = row_bcast<I0 + i>(w);
                 v[i] = make_uint4(0, 0, 0, 0);
                 if (t >= 0) v[i] = *reinterpret_cast<const uint4 *>(at + (int64_t)t * p.ld);
-            }
-#pragma unroll
-            for (int i = 0; i < AP_EMBED_AHEAD; i++) {
+            });
+            for_each_const<AP_EMBED_AHEAD>([&](auto i) {
                 float x[N];
                 ApRow16<DT>::get(v[i], x);
                 if (LISTS) {
 #pragma unroll
                     for (int j = 0; j < N; j++) sum[j] = fmaf(wi[i], x[j], sum[j]);
-                } else if (mine && i0 + i * 4 + g < count) {
+                } else if (mine && (I0 + i) * 4 + g < count) {
 #pragma unroll
                     for (int j = 0; j < N; j++) x[j] *= wi[i];
-                    put_row<OT, N>(p.out + (e + i0 + i * 4 + g) * p.dim * (OT == AP_F32 ? 4 : 2), col, x);
+                    put_row<OT, N>(p.out + (e + (I0 + i) * 4 + g) * p.dim * (OT == AP_F32 ? 4 : 2), col, x);
                 }
-            }
-        }
+            });
+        });
     }
     if (!LISTS) return;
 #pragma unroll
@@ -214,15 +225,25 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
         int64_t row = -1;
         float w = 0.f;
         if (same) { row = row_of(p.indptr, p.rows, e + lane); w = p.scale * (p.weights ? p.weights[e + lane] : 1.f); }
-        for (uint64_t m = __ballot(row >= 0); m; m &= m - 1) {
-            const int k = __ffsll((unsigned long long)m) - 1;
-            const int64_t r = (int64_t)__shfl((unsigned long long)row, k, 64);
-            const float wk = __shfl(w, k, 64);
-            if (group < groups) {
-                float x[N];
-                ApRow16<GT>::get(*reinterpret_cast<const uint4 *>(p.table + r * p.ld + group * 16), x);
+        for (uint64_t m = __ballot(row >= 0); m;) {   // eight rows on their way at a time: a frequent token has many
+            uint4 v[8];
+            float wk[8];
 #pragma unroll
-                for (int j = 0; j < N; j++) sum[j] = fmaf(wk, x[j], sum[j]);
+            for (int i = 0; i < 8; i++) {
+                v[i] = make_uint4(0, 0, 0, 0);
+                wk[i] = 0.f;
+                if (!m) continue;
+                const int k = __ffsll((unsigned long long)m) - 1;
+                m &= m - 1;
+                wk[i] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k));
+                if (group < groups) v[i] = *reinterpret_cast<const uint4 *>(p.table + (int64_t)__builtin_amdgcn_readlane((int32_t)row, k) * p.ld + group * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                float x[N];
+                ApRow16<GT>::get(v[i], x);
+#pragma unroll
+                for (int j = 0; j < N; j++) sum[j] = fmaf(wk[i], x[j], sum[j]);
             }
         }
     }
@@ -262,9 +283,19 @@ __global__ __launch_bounds__(256) void k_sort_scan(uint32_t *__restrict__ hist, 
     }
     if (lane == 0) totals[bin] = before;
 }
-// The list of every entry.
+// The list of every entry: 16 lanes a list.  Entries of none keep the -1 that is there.
 __global__ __launch_bounds__(256) void k_sort_rows(ApEmbed p, int32_t *__restrict__ row) {
-    for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < p.n; e += (int64_t)gridDim.x * 256) row[e] = (int32_t)row_of(p.indptr, p.rows, e);
+    for (int64_t r = blockIdx.x * (int64_t)16 + (threadIdx.x >> 4); r < p.rows; r += (int64_t)gridDim.x * 16) {
+        if (!ap_row_ok(p.indptr, r, p.n)) continue;
+        const int64_t end = p.indptr[r + 1];
+        for (int64_t e = p.indptr[r] + (threadIdx.x & 15); e < end; e += 16) row[e] = (int32_t)r;
+    }
+}
+static int list_rows(const ApEmbed &p, int32_t *row, hipStream_t st) {
+    AP_TRY(ap_fill_u32(row, (size_t)p.n, 0xffffffffu, st));
+    hipLaunchKernelGGL(k_sort_rows, dim3((unsigned)std::min<int64_t>((p.rows + 15) / 16, 8192)), dim3(256), 0, st, p, row);
+    AP_CHECK_HIP(hipGetLastError());
+    return AP_OK;
 }
 // The last pass also brings along what the sums need of an entry: its row (-1: none) and its weight.
 __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t *__restrict__ keys, const int32_t *__restrict__ entries, int shift, int bits, const uint32_t *__restrict__ hist,
@@ -340,28 +371,26 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, Ap
         const uint32_t key = is ? s.keys[e + l16] : 0xffffffffu;
         const uint32_t next = e + l16 + 1 < p.n ? s.keys[e + l16 + 1] : 0xffffffffu;
         const int32_t row = is && key < p.vocab ? s.rows[e + l16] : -1;   // -1 also for an entry of no list
-        const float w = is ? s.w[e + l16] : 0.f;
+        const float w = row >= 0 ? s.w[e + l16] : 0.f;
         // 1: the token's sum ends here, 2: it goes on in the next run
         const int32_t what = is && key < p.vocab ? (next != key ? 1 : e + l16 + 1 == end ? 2 : 0) : 0;
-#pragma unroll
-        for (int k0 = 0; k0 < 16; k0 += 8) {
+        for_each_const<2>([&](auto half) {
+            constexpr int K0 = decltype(half)::value * 8;
             uint4 v[8];
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                const int32_t r = __shfl(row, k0 + k, 16);
+            for_each_const<8>([&](auto k) {
+                const int32_t r = row_bcast<K0 + k>(row);
                 v[k] = make_uint4(0, 0, 0, 0);
                 if (r >= 0) v[k] = *reinterpret_cast<const uint4 *>(at + (int64_t)r * p.ld);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                const float wk = __shfl(row, k0 + k, 16) >= 0 ? __shfl(w, k0 + k, 16) : 0.f;
-                const int32_t end_k = __shfl(what, k0 + k, 16);
-                const uint32_t t = __shfl(key, k0 + k, 16);
+            });
+            for_each_const<8>([&](auto k) {
+                const float wk = row_bcast<K0 + k>(w);
                 float x[N];
                 ApRow16<GT>::get(v[k], x);
 #pragma unroll
                 for (int j = 0; j < N; j++) sum[j] = fmaf(wk, x[j], sum[j]);
-                if (!end_k) continue;
+                const int32_t end_k = row_bcast<K0 + k>(what);
+                if (!end_k) return;
+                const int32_t t = row_bcast<K0 + k>((int32_t)key);
                 if (mine) {
                     if (begun) put_row<AP_F32, N>(s.carry + run * 2 * p.dim, col, sum);
                     else if (end_k == 2) put_row<AP_F32, N>(s.carry + (run * 2 + 1) * p.dim, col, sum);
@@ -370,42 +399,61 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, Ap
 #pragma unroll
                 for (int j = 0; j < N; j++) sum[j] = 0.f;
                 begun = false;
-            }
-        }
+            });
+        });
     }
 }
-// One block for each run whose last token goes on: adds up the sums of the runs that it lies in.  16 waves share them.
+// A wave for each run whose last token goes on adds up the sums of the runs that it lies in; the four waves of a workgroup share the runs of a
+// token that lies in many.
+#define AP_JOIN_ALONE 32
 template <int OT>
-__global__ __launch_bounds__(1024) void k_embed_grad_join(ApEmbed p, ApRuns s, int64_t runs) {
-    __shared__ float4 s_sum[16][64];
-    const int64_t run = blockIdx.x, last = run * s.run + s.run - 1;   // the run's last entry
-    if (last + 1 >= p.n) return;
-    const uint32_t t = s.keys[last];
-    if (t >= p.vocab || s.keys[last + 1] != t) return;                     // it ends here
-    if (run > 0 && s.keys[run * s.run] == t && s.keys[run * s.run - 1] == t) return;   // it began earlier
-    int64_t lo = run + 1, hi = runs;   // the runs that begin with t: run + 1 .. lo - 1
-    while (lo < hi) { const int64_t m = (lo + hi) / 2; if (s.keys[m * s.run] == t) lo = m + 1; else hi = m; }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t each = (lo - run - 1 + 15) / 16, b = run + 1 + wave * each, end = min(lo, b + each);
+__global__ __launch_bounds__(256) void k_embed_grad_join(ApEmbed p, ApRuns s, int64_t runs) {
+    __shared__ float4 s_sum[4][64];
+    __shared__ int64_t s_lo[4];
+    const int lane = threadIdx.x & 63, wave = ap_wave_id();
+    const int64_t first = (int64_t)blockIdx.x * 4, run = first + wave, last = run * s.run + s.run - 1;   // the run's last entry
+    int64_t lo = 0;   // the runs that begin with its token: run + 1 .. lo - 1; 0: nothing to do
+    if (last + 1 < p.n) {
+        const uint32_t t = s.keys[last];
+        if (t < p.vocab && s.keys[last + 1] == t && !(run > 0 && s.keys[run * s.run] == t && s.keys[run * s.run - 1] == t)) {   // goes on, and began here
+            lo = run + 1;
+            for (int64_t hi = runs; lo < hi;) { const int64_t m = (lo + hi) / 2; if (s.keys[m * s.run] == t) lo = m + 1; else hi = m; }
+        }
+    }
+    if (lane == 0) s_lo[wave] = lo;
+    __syncthreads();
     for (int c0 = blockIdx.y * 64; c0 * 4 < p.dim; c0 += gridDim.y * 64) {
         const int c = (c0 + lane) * 4;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < p.dim) {
-            if (wave == 0) sum = *reinterpret_cast<const float4 *>(s.carry + (run * 2 + 1) * p.dim + c);
+        auto add = [&](int64_t b, int64_t end, float4 sum) {
 #pragma unroll 8
             for (int64_t r = b; r < end; r++) {
                 const float4 v = *reinterpret_cast<const float4 *>(s.carry + r * 2 * p.dim + c);
                 sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
             }
-        }
-        s_sum[wave][lane] = sum;
-        __syncthreads();
-        if (wave == 0 && c < p.dim) {
-            for (int w = 1; w < 16; w++) { const float4 v = s_sum[w][lane]; sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; }
+            return sum;
+        };
+        auto put = [&](int64_t of, const float4 &sum) {
             const float v[4] = {sum.x, sum.y, sum.z, sum.w};
-            put_row<OT, 4>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), c, v);
+            put_row<OT, 4>(p.out + (int64_t)s.keys[of * s.run + s.run - 1] * p.dim * (OT == AP_F32 ? 4 : 2), c, v);
+        };
+        for (int w = 0; w < 4; w++) {
+            const int64_t of = first + w, to = s_lo[w], count = to - of - 1;
+            if (to == 0 || (count <= AP_JOIN_ALONE && w != wave)) continue;
+            if (count <= AP_JOIN_ALONE) {
+                if (c < p.dim) put(of, add(of + 1, to, *reinterpret_cast<const float4 *>(s.carry + (of * 2 + 1) * p.dim + c)));
+                continue;
+            }
+            const int64_t each = (count + 3) / 4, b = of + 1 + wave * each;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c < p.dim) sum = add(b, min(to, b + each), wave ? sum : *reinterpret_cast<const float4 *>(s.carry + (of * 2 + 1) * p.dim + c));
+            s_sum[wave][lane] = sum;
+            __syncthreads();
+            if (wave == 0 && c < p.dim) {
+                for (int k = 1; k < 4; k++) { const float4 v = s_sum[k][lane]; sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; }
+                put(of, sum);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -431,6 +479,8 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
     const int32_t col = (slab * 16 + l16) * N;
     const bool mine = col < p.dim;
     const char *a = p.table + (mine ? col : 0) * (DT == AP_F32 ? 4 : 2), *b = g + (mine ? col : 0) * (GT == AP_F32 ? 4 : 2);
+    const int32_t first = __builtin_amdgcn_readfirstlane(row);
+    const bool same = first >= 0 && __all(row == first || tok < 0);   // one list, as most often: its gradient is read once
     float sum[4];
     uint4 x[4], y[4];
     bool used[4];
@@ -442,7 +492,14 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
         if (!used[i]) continue;
         const char *pa = a + (int64_t)t * p.ld, *pb = b + (int64_t)r * ldg;
         if (DT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pa); x[i].x = v.x; x[i].y = v.y; } else x[i] = *reinterpret_cast<const uint4 *>(pa);
+        if (same) continue;
         if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pb); y[i].x = v.x; y[i].y = v.y; } else y[i] = *reinterpret_cast<const uint4 *>(pb);
+    }
+    if (same && mine) {
+        const char *pb = b + (int64_t)first * ldg;
+        if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pb); y[0].x = v.x; y[0].y = v.y; } else y[0] = *reinterpret_cast<const uint4 *>(pb);
+#pragma unroll
+        for (int i = 1; i < 4; i++) y[i] = y[0];
     }
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -452,6 +509,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
         sum[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < N; j++) sum[i] = fmaf(u[j], v[j], sum[i]);
+        if (!used[i]) sum[i] = 0.f;   // NaN of a list that it is not in
         sum[i] += ap_dpp<0xB1>(sum[i]);
         sum[i] += ap_dpp<0x4E>(sum[i]);
         sum[i] += ap_dpp<0x141>(sum[i]);
@@ -586,7 +644,7 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
 #undef AP_FEW
         return AP_OK;
     }
-    if (lists->indptr) hipLaunchKernelGGL(k_sort_rows, dim3((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192)), dim3(256), 0, st, p, ws.rows_in);
+    if (lists->indptr) AP_TRY(list_rows(p, ws.rows_in, st));
     for (int i = 0; i < ws.passes; i++) {
         const uint32_t *keys = i ? ws.keys[(i - 1) & 1] : nullptr;
         const int32_t *entries = i ? ws.entries[(i - 1) & 1] : nullptr;
@@ -599,12 +657,12 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     const ApRuns s{ws.keys[(ws.passes - 1) & 1], ws.rows, ws.w, ws.carry, ws.run};
     const ApSlabs sl = slabs_of((int64_t)dim * (dtype == AP_BF16 ? 2 : 4), div_up(ws.runs, 16));
     AP_REQUIRE(slab_blocks(sl) < (1ll << 23), "too many entries");
-    const dim3 grid((unsigned)slab_blocks(sl)), joins((unsigned)ws.runs, (unsigned)std::max<int64_t>(1, std::min<int64_t>(div_up(dim, 256), (1ll << 21) / ws.runs)));   // below 2^31 threads
+    const dim3 grid((unsigned)slab_blocks(sl)), joins((unsigned)div_up(ws.runs, 4), (unsigned)std::max<int64_t>(1, std::min<int64_t>(div_up(dim, 256), (1ll << 25) / ws.runs)));   // below 2^31 threads
 #define AP_RUNS(A, B) hipLaunchKernelGGL((k_embed_grad_runs<A, B>), grid, dim3(256), 0, st, p, s, sl)
     AP_TYPES(dtype, table_dtype, AP_RUNS);
 #undef AP_RUNS
-    if (table_dtype == AP_F32) hipLaunchKernelGGL((k_embed_grad_join<AP_F32>), joins, dim3(1024), 0, st, p, s, ws.runs);
-    else hipLaunchKernelGGL((k_embed_grad_join<AP_BF16>), joins, dim3(1024), 0, st, p, s, ws.runs);
+    if (table_dtype == AP_F32) hipLaunchKernelGGL((k_embed_grad_join<AP_F32>), joins, dim3(256), 0, st, p, s, ws.runs);
+    else hipLaunchKernelGGL((k_embed_grad_join<AP_BF16>), joins, dim3(256), 0, st, p, s, ws.runs);
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }
@@ -648,7 +706,7 @@ extern "C" int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t 
     const dim3 grid((unsigned)slab_blocks(s)), flat((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192));
     float *parts = slabs > 1 ? static_cast<float *>(workspace) : grad_weights;
     int32_t *rows = lists->indptr && row_bytes ? reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + part_bytes) : nullptr;
-    if (rows) hipLaunchKernelGGL(k_sort_rows, flat, dim3(256), 0, st, p, rows);
+    if (rows) AP_TRY(list_rows(p, rows, st));
 #define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(256), 0, st, p, s, rows, g, ldb, parts)
     AP_TYPES(dtype, grad_dtype, AP_WEIGHTS);
 #undef AP_WEIGHTS
