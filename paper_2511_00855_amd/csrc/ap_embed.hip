@@ -458,7 +458,8 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(ApEmbed p, ApRuns s, in
 }
 
 // ------------------------------------------------------------------ gradient of the weights
-// 16 lanes take an entry and a slab of it; a wave 16 entries in a row.  A slab's part goes to out[slab][entry].
+// 16 lanes take 16 entries in a row and a slab of them; the gradient of a list stays in registers while its entries last.  A slab's part goes to
+// out[slab][entry].
 template <int DT, int GT>
 __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s, const int32_t *__restrict__ rows /* of every entry; NULL: looked up */, const char *__restrict__ g, int64_t ldg,
                                                             float *__restrict__ out) {
@@ -467,56 +468,52 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
     int32_t slab;
     int64_t unit;
     if (!slab_block(s, &slab, &unit)) return;
-    const int lane = threadIdx.x & 63, l16 = lane & 15;
-    const int64_t e0 = (unit * 4 + (threadIdx.x >> 6)) * 16;
-    if (e0 >= p.n) return;
+    const int l16 = threadIdx.x & 15;
+    const int64_t e = unit * 256 + threadIdx.x;   // this lane's entry
     int32_t row = -1, tok = -1;
-    if (e0 + l16 < p.n) {
-        tok = p.tokens[e0 + l16];
+    if (e < p.n) {
+        tok = p.tokens[e];
         if (tok >= p.vocab) tok = -1;
-        if (tok >= 0) row = rows ? rows[e0 + l16] : (int32_t)row_of(p.indptr, p.rows, e0 + l16);
+        if (tok >= 0) row = rows ? rows[e] : (int32_t)row_of(p.indptr, p.rows, e);
     }
     const int32_t col = (slab * 16 + l16) * N;
     const bool mine = col < p.dim;
     const char *a = p.table + (mine ? col : 0) * (DT == AP_F32 ? 4 : 2), *b = g + (mine ? col : 0) * (GT == AP_F32 ? 4 : 2);
-    const int32_t first = __builtin_amdgcn_readfirstlane(row);
-    const bool same = first >= 0 && __all(row == first || tok < 0);   // one list, as most often: its gradient is read once
-    float sum[4];
-    uint4 x[4], y[4];
-    bool used[4];
+    float own = 0.f;   // what this lane's entry gets
+    uint4 last = make_uint4(0, 0, 0, 0);
+    int32_t last_row = -1;
+    for_each_const<4>([&](auto batch) {
+        constexpr int K0 = decltype(batch)::value * 4;
+        uint4 x[4], y[4];
+        int32_t r[4];
+        for_each_const<4>([&](auto i) {
+            const int32_t t = row_bcast<K0 + i>(tok);
+            r[i] = row_bcast<K0 + i>(row);
+            x[i] = y[i] = make_uint4(0, 0, 0, 0);
+            if (r[i] < 0) return;
+            const char *pa = a + (int64_t)t * p.ld;
+            if (DT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pa); x[i].x = v.x; x[i].y = v.y; } else x[i] = *reinterpret_cast<const uint4 *>(pa);
+            if (r[i] == (i ? r[i ? i - 1 : 0] : last_row)) return;
+            const char *pb = b + (int64_t)r[i] * ldg;
+            if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pb); y[i].x = v.x; y[i].y = v.y; } else y[i] = *reinterpret_cast<const uint4 *>(pb);
+        });
+        for_each_const<4>([&](auto i) {
+            if (r[i] != last_row) last = y[i];   // zeros for an entry of no list
+            last_row = r[i];
+            float u[8], v[8], sum = 0.f;
+            ApRow16<DT>::get(x[i], u);
+            ApRow16<GT>::get(last, v);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {   // entry 4 i + lane / 16
-        const int32_t t = __shfl(tok, i * 4 + (lane >> 4), 64), r = __shfl(row, i * 4 + (lane >> 4), 64);
-        used[i] = r >= 0 && mine;
-        x[i] = y[i] = make_uint4(0, 0, 0, 0);
-        if (!used[i]) continue;
-        const char *pa = a + (int64_t)t * p.ld, *pb = b + (int64_t)r * ldg;
-        if (DT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pa); x[i].x = v.x; x[i].y = v.y; } else x[i] = *reinterpret_cast<const uint4 *>(pa);
-        if (same) continue;
-        if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pb); y[i].x = v.x; y[i].y = v.y; } else y[i] = *reinterpret_cast<const uint4 *>(pb);
-    }
-    if (same && mine) {
-        const char *pb = b + (int64_t)first * ldg;
-        if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(pb); y[0].x = v.x; y[0].y = v.y; } else y[0] = *reinterpret_cast<const uint4 *>(pb);
-#pragma unroll
-        for (int i = 1; i < 4; i++) y[i] = y[0];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        float u[8], v[8];
-        ApRow16<DT>::get(x[i], u);
-        ApRow16<GT>::get(y[i], v);
-        sum[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < N; j++) sum[i] = fmaf(u[j], v[j], sum[i]);
-        if (!used[i]) sum[i] = 0.f;   // NaN of a list that it is not in
-        sum[i] += ap_dpp<0xB1>(sum[i]);
-        sum[i] += ap_dpp<0x4E>(sum[i]);
-        sum[i] += ap_dpp<0x141>(sum[i]);
-        sum[i] += ap_dpp<0x140>(sum[i]);
-        const int64_t e = e0 + i * 4 + (lane >> 4);
-        if (l16 == 0 && e < p.n) out[slab * p.n + e] = sum[i] * p.scale;
-    }
+            for (int j = 0; j < N; j++) sum = fmaf(u[j], v[j], sum);
+            sum = mine ? sum : 0.f;
+            sum += ap_dpp<0xB1>(sum);
+            sum += ap_dpp<0x4E>(sum);
+            sum += ap_dpp<0x141>(sum);
+            sum += ap_dpp<0x140>(sum);
+            if (l16 == K0 + i) own = sum;
+        });
+    });
+    if (e < p.n) out[slab * p.n + e] = own * p.scale;
 }
 __global__ __launch_bounds__(256) void k_embed_grad_weights_sum(const float *__restrict__ parts, int64_t n, int32_t slabs, float *__restrict__ out) {
     for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
@@ -582,6 +579,9 @@ extern "C" int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vo
     return AP_OK;
 }
 
+#ifndef AP_RUNS
+#define AP_RUNS 16384
+#endif
 struct GradWs {
     int64_t blocks, runs;
     int32_t run, passes, bits;
@@ -597,7 +597,7 @@ struct GradWs {
         bits = (int32_t)div_up(all, passes);
         blocks = div_up(n, AP_SORT_ITEMS);
         run = 64;   // as long as they fill the compute units: every run leaves two rows of sums behind
-        while (run < 256 && n / run > 8192) run *= 2;
+        while (run < 256 && n / run > AP_RUNS) run *= 2;
         runs = div_up(n, run);
         for (int i = 0; i < 2; i++) { keys[i] = (uint32_t *)take(n); entries[i] = (int32_t *)take(n); }
         hist = (uint32_t *)take(blocks << bits);
@@ -701,7 +701,7 @@ extern "C" int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t 
     const ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, nullptr);
     const char *g = static_cast<const char *>(grad_out);
     const int64_t ldb = ldg * (grad_dtype == AP_BF16 ? 2 : 4);
-    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, 64));
+    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, 256));
     AP_REQUIRE(slab_blocks(s) < (1ll << 23), "too many entries");
     const dim3 grid((unsigned)slab_blocks(s)), flat((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192));
     float *parts = slabs > 1 ? static_cast<float *>(workspace) : grad_weights;
