@@ -115,7 +115,7 @@ def debug_set(name: str, value: int):
 
 DEBUG_NAMES = ("seed_sample_cols", "seed_buffer_cap", "seed_tau_ulps", "max_launch_threads", "search_workspace_bytes",
                "search_visited_global", "search_query_lists", "seed_one_sided", "search_bounds", "search_walk", "search_bounds_bytes", "search_floor", "prune_walks",
-               "bound_buckets", "loss_piece", "embed_few")
+               "bound_buckets", "loss_piece", "loss_form", "embed_few")
 
 
 def debug_reset():
@@ -549,14 +549,16 @@ def _vec(t: torch.Tensor, dtype, count: int, device, what: str):
 
 def _call(fn: str, device, *args, bytes_args=None):
     """Calls ap_<fn> on the device's current stream, with the workspace that ap_<fn>_bytes(*bytes_args) asks for."""
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _call(fn, device, *args, bytes_args=bytes_args)
     L = lib()
-    with torch.cuda.device(device):
-        if bytes_args is not None:
-            need = C.c_size_t()
-            _check(getattr(L, fn + "_bytes")(*bytes_args, C.byref(need)), fn + "_bytes")
-            ws = torch.empty(need.value, dtype=torch.uint8, device=device)
-            args += (ws.data_ptr(), need.value)
-        _check(getattr(L, fn)(*args, torch.cuda.current_stream().cuda_stream), fn)
+    if bytes_args is not None:
+        need = C.c_size_t()
+        _check(getattr(L, fn + "_bytes")(*bytes_args, C.byref(need)), fn + "_bytes")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None   # held until the call has been made
+        args += (None if ws is None else ws.data_ptr(), need.value)
+    _check(getattr(L, fn)(*args, torch._C._cuda_getCurrentRawStream(device.index)), fn)
 
 
 def _same(a: torch.Tensor, b: torch.Tensor, what: str):

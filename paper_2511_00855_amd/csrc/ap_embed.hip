@@ -204,7 +204,16 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
         }
         return;
     }
-    for (int i = threadIdx.x; i < p.n; i += 256) s_few[i] = p.tokens[i];
+    // the tokens and, of each, its list: looked up when a token has been found would be a chain of reads for every 64 entries
+    int32_t *s_row = s_few + p.n;
+    for (int i = threadIdx.x; i < p.n; i += 256) { s_few[i] = p.tokens[i]; s_row[i] = p.indptr ? -1 : i; }
+    __syncthreads();
+    if (p.indptr)
+        for (int64_t r = threadIdx.x >> 4; r < p.rows; r += 16) {
+            if (!ap_row_ok(p.indptr, r, p.n)) continue;
+            const int end = (int)p.indptr[r + 1];
+            for (int e = (int)p.indptr[r] + (threadIdx.x & 15); e < end; e += 16) s_row[e] = (int32_t)r;
+        }
     __syncthreads();
     const int groups = p.dim / N, slabs = (groups + 63) / 64;
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
         if (!__any(same)) continue;
         int64_t row = -1;
         float w = 0.f;
-        if (same) { row = row_of(p.indptr, p.rows, e + lane); w = p.scale * (p.weights ? p.weights[e + lane] : 1.f); }
+        if (same) { row = s_row[e + lane]; w = p.scale * (p.weights ? p.weights[e + lane] : 1.f); }
         for (uint64_t m = __ballot(row >= 0); m;) {   // eight rows on their way at a time: a frequent token has many
             uint4 v[8];
             float wk[8];
@@ -469,7 +478,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
     int64_t unit;
     if (!slab_block(s, &slab, &unit)) return;
     const int l16 = threadIdx.x & 15;
-    const int64_t e = unit * 256 + threadIdx.x;   // this lane's entry
+    const int64_t e = unit * blockDim.x + threadIdx.x;   // this lane's entry
     int32_t row = -1, tok = -1;
     if (e < p.n) {
         tok = p.tokens[e];
@@ -637,7 +646,7 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     if (!any) return AP_OK;
     if (few) {
         const int32_t owners = (int32_t)div_up(lists->n * div_up(dim / (dtype == AP_BF16 ? 8 : 4), 64), 4), bits = one ? (int32_t)vocab : 0;
-        const size_t lds = std::max<size_t>((size_t)lists->n * 4, (size_t)(bits + 31) / 32 * 4);
+        const size_t lds = std::max<size_t>((size_t)lists->n * 8, (size_t)(bits + 31) / 32 * 4);
         const dim3 grid((unsigned)(owners + (one ? std::min<int64_t>(div_up(words, 1024), 1024) : 0)));
 #define AP_FEW(A, B) hipLaunchKernelGGL((k_embed_grad_few<A, B>), grid, dim3(256), lds, st, p, owners, bits)
         AP_TYPES(dtype, table_dtype, AP_FEW);
@@ -701,13 +710,14 @@ extern "C" int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t 
     const ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, nullptr);
     const char *g = static_cast<const char *>(grad_out);
     const int64_t ldb = ldg * (grad_dtype == AP_BF16 ? 2 : 4);
-    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, 256));
+    const unsigned threads = lists->n > (1 << 14) ? 256 : 64;   // few entries: as many workgroups as there can be
+    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, threads));
     AP_REQUIRE(slab_blocks(s) < (1ll << 23), "too many entries");
     const dim3 grid((unsigned)slab_blocks(s)), flat((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192));
     float *parts = slabs > 1 ? static_cast<float *>(workspace) : grad_weights;
     int32_t *rows = lists->indptr && row_bytes ? reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + part_bytes) : nullptr;
     if (rows) AP_TRY(list_rows(p, rows, st));
-#define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(256), 0, st, p, s, rows, g, ldb, parts)
+#define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(threads), 0, st, p, s, rows, g, ldb, parts)
     AP_TYPES(dtype, grad_dtype, AP_WEIGHTS);
 #undef AP_WEIGHTS
     if (slabs > 1) hipLaunchKernelGGL(k_embed_grad_weights_sum, flat, dim3(256), 0, st, parts, lists->n, slabs, grad_weights);

@@ -1,5 +1,5 @@
 // The tile product under the losses and the 8-bit scores: C[m][n] = sum_k A[m][k] B[n][k] of one workgroup's tile, on
-// the matrix instructions of gfx950, for 16-bit floats (bf16, f16; sums in f32) and 8-bit integers (sums in i32, exact).
+// the matrix instructions of gfx950, for 16-bit floats (bf16, f16) and f32 (sums in f32) and 8-bit integers (sums in i32, exact).
 //
 // An operand lies in memory either with k running along its rows (a row of A is a line of memory) or with k running from
 // line to line; a product takes any pair of the two, so that neither a gradient's operand nor its result is transposed
@@ -30,6 +30,17 @@ struct ApF16Op {
     static constexpr int BYTES = 2;
     static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(ap_g_f16x8, a), __builtin_bit_cast(ap_g_f16x8, b), c, 0, 0, 0);
+    }
+};
+// f32 rows as they are: four instructions of 4 values of k for a lane's 16 bytes, a sixteenth of the others' rate.
+struct ApF32Op {
+    typedef ap_g_f32x4 Acc;
+    static constexpr int BYTES = 4;
+    static __device__ __forceinline__ Acc mul(ap_g_i32x4 a, ap_g_i32x4 b, Acc c) {
+        const ap_g_f32x4 x = __builtin_bit_cast(ap_g_f32x4, a), y = __builtin_bit_cast(ap_g_f32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; i++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+        return c;
     }
 };
 struct ApI8Op {
@@ -78,9 +89,11 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
 
     // Chunks of 16 bytes change places within a line of LDS, so that the 16 lanes that are served at a time fall in different banks.  Lines of k: 16
     // rows are read at the same chunk, and two rows fill the 256 bytes of all banks.  Lines of rows or columns: 32 lanes read 32 bytes of
-    // each of the lines k, .. k + 3, k + 8, .. k + 11.
+    // each of the lines k, .. k + 3, k + 8, .. k + 11 (f32: 64 lanes 64 bytes of the lines k, k + 4, k + 8, k + 12).
     static __device__ __forceinline__ int swap_k(int row) { return (row >> 1) & 7; }
-    static __device__ __forceinline__ int swap_t(int k, int t) { return (((k & 3) | ((k >> 1) & 4)) * 2) & (t * OP::BYTES / 16 - 1); }
+    static __device__ __forceinline__ int swap_t(int k, int t) {
+        return (OP::BYTES == 4 ? (k & 12) : ((k & 3) | ((k >> 1) & 4)) * 2) & (t * OP::BYTES / 16 - 1);
+    }
 
     // The offsets, relative to a chunk's first byte, of what this lane brings of an operand of T rows.
     template <int T, bool LINE>
@@ -115,12 +128,18 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
     // The 16 bytes of k that this lane feeds to step `step` for the 16 rows from `row` on: k from 16 (lane / 16) bytes on, of row lane % 16.
     template <int T, bool LINE>
     static __device__ __forceinline__ ap_g_i32x4 frag(const char *lds, int row, int step, int lane) {
-        if (LINE) {
+        if constexpr (LINE) {
             const int r = row + (lane & 15), chunk = (step * 4 + (lane >> 4)) ^ swap_k(r);
             return *reinterpret_cast<const ap_g_i32x4 *>(lds + r * AP_G_LINE + chunk * 16);
+        } else if constexpr (OP::BYTES == 4) {
+            const int k = step * 16 + (lane >> 4) * 4, col = row + (lane & 15);
+            ap_g_i32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] = *reinterpret_cast<const int32_t *>(lds + (k + i) * (T * 4) + (((col >> 2) ^ swap_t(k + i, T)) << 4) + (col & 3) * 4);
+            return v;
         } else {
             // 16 lanes read 4 lines of 16 columns and get 4 values of k of a column each
-            static_assert(LINE || OP::BYTES == 2, "lines of rows are of 16-bit values");
+            static_assert(LINE || OP::BYTES == 2, "lines of rows are of 16-bit or f32 values");
             const int k = step * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3), col = (row + (lane & 3) * 4) * 2;
             ap_g_s16x4 v[2];
 #pragma unroll
@@ -198,6 +217,11 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
 #pragma unroll
             for (int i = 0; i < NR; i++) read1(0, 0, 0, i);
         }
+        // f32 products add four values of k at a time: sums of 256 are added up apart, or a long sum would be off by the root of its length
+        Acc total[OP::BYTES == 4 ? FA : 1][OP::BYTES == 4 ? FB : 1];
+        if constexpr (OP::BYTES == 4)
+#pragma unroll
+            for (int i = 0; i < NM; i++) total[i / FB][i % FB] = Acc{0, 0, 0, 0};
         for (int32_t c = 0; c < chunks; c++) {
             const int st = c & 1;
             mul(0, [&](int i) {   // the reads in the first half
@@ -220,7 +244,14 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
                 }
             });
             advance();
+            if constexpr (OP::BYTES == 4)
+                if ((c & 7) == 7 || c + 1 == chunks)
+#pragma unroll
+                    for (int i = 0; i < NM; i++) { total[i / FB][i % FB] += acc[i / FB][i % FB]; acc[i / FB][i % FB] = Acc{0, 0, 0, 0}; }
         }
+        if constexpr (OP::BYTES == 4)
+#pragma unroll
+            for (int i = 0; i < NM; i++) acc[i / FB][i % FB] = total[i / FB][i % FB];
         ap_g_wait_loads<0>();
         ap_g_barrier();   // the stages may be used for something else
     }

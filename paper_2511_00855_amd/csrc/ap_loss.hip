@@ -23,7 +23,6 @@
 #define AP_COEF_UP 14                            // f16 coefficients are stored times 2^14: they are at most 1
 
 // ------------------------------------------------------------------ f32 rows as two f16 parts
-// Largest finite magnitude of two arrays of rows, as the bits of a float (which are in the order of the numbers).
 struct ApSide { const float *p; int64_t ld, rows; };
 // Four 16-byte groups of a matrix of `total` at once: group i + k * step of it, or nothing past the end.
 __device__ __forceinline__ void ap_load4(const ApSide &s, int32_t per, int64_t total, int64_t i, int64_t step, float4 (&v)[4]) {
@@ -34,7 +33,9 @@ __device__ __forceinline__ void ap_load4(const ApSide &s, int32_t per, int64_t t
         if (at < total) v[k] = *reinterpret_cast<const float4 *>(s.p + (s.ld == per * 4 ? at * 4 : at / per * s.ld + at % per * 4));
     }
 }
-__global__ __launch_bounds__(256) void k_loss_amax(ApSide a, ApSide b, int32_t dim, uint32_t *__restrict__ out /* [2], zero */) {
+// Largest finite magnitude of two arrays, a number of every workgroup: the bits of a float, which are in the order of the numbers.
+#define AP_LOSS_AMAX 2048
+__global__ __launch_bounds__(256) void k_loss_amax(ApSide a, ApSide b, int32_t dim, uint32_t *__restrict__ out /* [2][gridDim.x] */) {
     __shared__ float s_m[4];
     const int32_t per = dim / 4;
     for (int side = 0; side < 2; side++) {
@@ -54,27 +55,37 @@ __global__ __launch_bounds__(256) void k_loss_amax(ApSide a, ApSide b, int32_t d
         for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
         if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
         __syncthreads();
-        if (threadIdx.x == 0) {   // one atomic a block, and none that would change nothing: thousands on one address cost as much as the reads
-            m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-            if (__float_as_uint(m) > *(volatile uint32_t *)&out[side]) atomicMax(&out[side], __float_as_uint(m));
-        }
+        if (threadIdx.x == 0) out[side * gridDim.x + blockIdx.x] = __float_as_uint(fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3])));
         __syncthreads();
     }
 }
 // The power of two that brings a largest magnitude into [2^14, 2^15).
 __device__ __forceinline__ int ap_loss_up(uint32_t amax) { return amax ? 14 - ilogbf(__uint_as_float(amax)) : 0; }
 
-// Rows in two f16 parts, `pad` columns each (zeros after the last).  Rows that `coef` gives 0 become zeros.
-__global__ __launch_bounds__(256) void k_loss_split(ApSide s, int32_t dim, int32_t pad, const uint32_t *__restrict__ amax, const float *__restrict__ coef,
-                                                    _Float16 *__restrict__ hi, _Float16 *__restrict__ lo) {
-    const int up = ap_loss_up(*amax);
+// Rows in two f16 parts, `pad` columns each (zeros after the last).  The first `blocks_a` workgroups take the documents, the others the queries; queries
+// that `coef` gives 0 become zeros.  amax: the numbers of k_loss_amax, `parts` of each side; their maxima go to `both`.
+__global__ __launch_bounds__(256) void k_loss_split(ApSide a, ApSide b, int32_t blocks_a, int32_t dim, int32_t pad, const uint32_t *__restrict__ amax, int32_t parts, uint32_t *__restrict__ both,
+                                                    const float *__restrict__ coef, _Float16 *__restrict__ out_a, _Float16 *__restrict__ out_b) {
+    __shared__ uint32_t s_m[4];
+    const int side = (int32_t)blockIdx.x >= blocks_a;
+    const ApSide s = side ? b : a;
+    uint32_t m = 0;
+    for (int i = threadIdx.x; i < parts; i += 256) m = max(m, amax[side * parts + i]);
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = max(max(s_m[0], s_m[1]), max(s_m[2], s_m[3]));
+    const int64_t block = side ? blockIdx.x - blocks_a : blockIdx.x;
+    if (block == 0 && threadIdx.x == 0) both[side] = m;
+    const int up = ap_loss_up(m);
     const int32_t per = pad / 4;
-    const int64_t total = s.rows * per, step = (int64_t)gridDim.x * 256;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += step) {
+    const int64_t total = s.rows * per, step = (int64_t)(side ? gridDim.x - blocks_a : blocks_a) * 256;
+    _Float16 *hi = side ? out_b : out_a, *lo = hi + s.rows * pad;
+    for (int64_t i = block * 256 + threadIdx.x; i < total; i += step) {
         const int64_t r = i / per;
         const int32_t c = (int32_t)(i - r * per) * 4;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < dim && (!coef || coef[r] != 0.f)) v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c);
+        if (c < dim && (!side || !coef || coef[r] != 0.f)) v = *reinterpret_cast<const float4 *>(s.p + r * s.ld + c);
         const float x[4] = {v.x, v.y, v.z, v.w};
         _Float16 h[4], l[4];
 #pragma unroll
@@ -102,7 +113,7 @@ struct ApLoss {
     float2 *part;                  // loss: [row tile][query] maximum, sum
     float *at_label;               // loss: the label's product
     const float *lse, *coef;       // gradient: of each query; g_q over the largest, 0 where it has no label
-    char *c;                       // gradient: coefficients [query][document of the piece]
+    char *c;                       // gradient: coefficients [query][document of the piece], of the products' type
     int64_t ldc, c_part;           // in bytes; c_part 0: coefficients of one part
 };
 
@@ -234,22 +245,23 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
     if (GRAD) {
         // a part of the coefficients goes through LDS, a query's documents together, and leaves in whole lines (four documents of a lane at a time
         // would write 32 bytes of 16 lines: a tile of 256 took half as long again); groups of 16 bytes change places by the query
-        constexpr int LINE = TM * 2, GROUPS = LINE / 16;
+        constexpr int LINE = TM * OP::BYTES, GROUPS = LINE / 16;
         for (int part = 0; part < (p.c_part ? 2 : 1); part++) {
 #pragma unroll
             for (int b = 0; b < G::FB; b++)
 #pragma unroll
                 for (int a = 0; a < G::FA; a++) {
-                    const int col = G::col(b), at = (row0 + a * 16) * 2, group = (at >> 4) ^ (col & (GROUPS < 16 ? GROUPS - 1 : 15));
+                    const int col = G::col(b), at = (row0 + a * 16) * OP::BYTES, group = (at >> 4) ^ (col & (GROUPS < 16 ? GROUPS - 1 : 15));
                     float v[4] = {acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]};
-                    *reinterpret_cast<uint2 *>(lds + col * LINE + group * 16 + (at & 15)) = ap_coef_part<PARTS>(v);
+                    if constexpr (OP::BYTES == 4) *reinterpret_cast<float4 *>(lds + col * LINE + group * 16) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *reinterpret_cast<uint2 *>(lds + col * LINE + group * 16 + (at & 15)) = ap_coef_part<PARTS>(v);
 #pragma unroll
                     for (int r = 0; r < 4; r++) acc[a][b][r] = v[r];   // what is left for the second part
                 }
             __syncthreads();
             for (int i = threadIdx.x; i < queries * GROUPS; i += G::THREADS) {
                 const int q = i / GROUPS, group = i % GROUPS;
-                *reinterpret_cast<uint4 *>(p.c + part * p.c_part + (int64_t)(n0 + q) * p.ldc + m0 * 2 + group * 16) =
+                *reinterpret_cast<uint4 *>(p.c + part * p.c_part + (int64_t)(n0 + q) * p.ldc + (int64_t)m0 * OP::BYTES + group * 16) =
                     *reinterpret_cast<const uint4 *>(lds + q * LINE + (group ^ (q & (GROUPS < 16 ? GROUPS - 1 : 15))) * 16);
             }
             __syncthreads();
@@ -347,9 +359,13 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
                     const float e = co.exp_of(f.of<false>(acc[g][r])) - (label[g] == p.first + d + r ? 1.f : 0.f);
                     v[r] = d + r < p.count ? co.times(e) : 0.f;
                 }
-                char *to = p.c + q * p.ldc + d * 2;
-                *reinterpret_cast<uint2 *>(to) = ap_coef_part<DT == AP_F32>(v);
-                if (p.c_part) *reinterpret_cast<uint2 *>(to + p.c_part) = ap_coef_part<DT == AP_F32>(v);
+                char *to = p.c + q * p.ldc + d * SIZE;
+                if constexpr (DT == AP_F32) {
+                    *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                } else {
+                    *reinterpret_cast<uint2 *>(to) = ap_coef_part<false>(v);
+                    if (p.c_part) *reinterpret_cast<uint2 *>(to + p.c_part) = ap_coef_part<false>(v);
+                }
             }
         });
         return;
@@ -390,30 +406,34 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
 }
 
 // ------------------------------------------------------------------ the gradients' products
-// *most = the largest |g_q| of the queries that have a label (1 if there is none): the coefficients are stored relative to it, so
-// that equal weights leave the label's own coefficient p - 1 without a rounding of the weight.
-__global__ __launch_bounds__(1024) void k_loss_most(const float *__restrict__ g, const int32_t *__restrict__ labels, int32_t rows, int32_t n, float *__restrict__ most,
-                                                    float *__restrict__ coef) {
+// *most = the largest |g_q| of the queries that have a label (1 if there is none): the coefficients are stored relative to it, so that equal weights
+// leave the label's own coefficient p - 1 without a rounding of the weight.  coef[q] = g_q / *most, 0 without a label.  With `out`, the queries too
+// (groups of 16 bytes), zeros for those of coefficient 0: what is multiplied by 0 must not be infinite or NaN.  Every workgroup finds the largest
+// by itself (up to AP_LOSS_PREP queries), or is told (`given`).
+#define AP_LOSS_PREP 16384
+__global__ __launch_bounds__(1024) void k_loss_prep(const float *__restrict__ g, const int32_t *__restrict__ labels, int32_t rows, int32_t n, const float *__restrict__ given,
+                                                    float *__restrict__ most, float *__restrict__ coef, const char *__restrict__ x, int64_t ld, int32_t groups, uint4 *__restrict__ out) {
     __shared__ float s_m[16];
     float m = 0.f;
-    for (int32_t q = threadIdx.x; q < rows; q += 1024)
-        if (labels[q] >= 0 && labels[q] < n) { const float v = fabsf(g[q]); m = v > m && v < INFINITY ? v : m; }
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = 0.f;
-    for (int w = 0; w < 16; w++) m = fmaxf(m, s_m[w]);
-    if (m == 0.f) m = 1.f;
-    if (threadIdx.x == 0) *most = m;
-    for (int32_t q = threadIdx.x; q < rows; q += 1024) coef[q] = labels[q] >= 0 && labels[q] < n ? g[q] / m : 0.f;
-}
-
-// bf16 queries without those that have no weight: what is multiplied by 0 must not be infinite or NaN
-__global__ __launch_bounds__(256) void k_loss_used(const char *__restrict__ x, int64_t ld, int32_t rows, int32_t groups, const float *__restrict__ coef, uint4 *__restrict__ out) {
+    if (given) m = *given;
+    else {
+        for (int32_t q = threadIdx.x; q < rows; q += 1024)
+            if (labels[q] >= 0 && labels[q] < n) { const float v = fabsf(g[q]); m = v > m && v < INFINITY ? v : m; }
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
+        __syncthreads();
+        m = 0.f;
+        for (int w = 0; w < 16; w++) m = fmaxf(m, s_m[w]);
+        if (m == 0.f) m = 1.f;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *most = m;
+    }
+    auto coef_of = [&](int64_t q) { return labels[q] >= 0 && labels[q] < n ? g[q] / m : 0.f; };
+    if (coef) for (int64_t q = blockIdx.x * (int64_t)1024 + threadIdx.x; q < rows; q += (int64_t)gridDim.x * 1024) coef[q] = coef_of(q);
+    if (!out) return;
     const int64_t total = (int64_t)rows * groups;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = blockIdx.x * (int64_t)1024 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 1024) {
         const int64_t r = i / groups, c = i % groups;
-        out[i] = coef[r] != 0.f ? *reinterpret_cast<const uint4 *>(x + r * ld + c * 16) : make_uint4(0, 0, 0, 0);
+        out[i] = coef_of(r) != 0.f ? *reinterpret_cast<const uint4 *>(x + r * ld + c * 16) : make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -438,6 +458,8 @@ struct ApLossGrad {
 
 template <class OP, int TM, int TN, int WM, int WN, bool PARTS>
 __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
+    constexpr int SIZE = OP::BYTES;
+    constexpr bool F32 = PARTS || SIZE == 4;
     using GD = ApGemm<OP, TM, TN, WM, WN, false, false>;
     using GX = ApGemm<OP, TM, TN, WM, WN, true, false>;
     __shared__ __attribute__((aligned(1024))) char lds[GD::LDS_BYTES];
@@ -449,7 +471,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
         const uint32_t run = m / mt, m0 = m % mt * TM, n0 = n * TN;
         const int32_t queries = min(TM, p.rows - (int32_t)m0), cols = min(TN, p.dim - (int32_t)n0);
         const int64_t d0 = (int64_t)run * p.run_docs, docs = min((int64_t)p.run_docs, p.count - d0);
-        GX::product({p.c + m0 * p.ldc + d0 * 2, p.ldc, queries}, {p.docs + (p.first + d0) * p.ldd + n0 * 2, p.ldd, cols * 2}, docs > 0 ? docs : 0, p.parts, p.c_part, p.d_part, lds, acc);
+        GX::product({p.c + m0 * p.ldc + d0 * SIZE, p.ldc, queries}, {p.docs + (p.first + d0) * p.ldd + n0 * SIZE, p.ldd, cols * SIZE}, docs > 0 ? docs : 0, p.parts, p.c_part, p.d_part, lds, acc);
         float *to = p.gx + ((int64_t)run * p.rows + m0) * p.dim + n0;
         // One workgroup of a launch adds to an element, and launches follow each other: the sums have one order, atomics or not.  They save the wait for
         // what is there.
@@ -460,14 +482,14 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
     uint32_t m, n;
     ap_g_tile(blockIdx.x - p.runs * mt * nt, (p.count + TM - 1) / TM, nt, nt, &m, &n);
     const int32_t m0 = m * TM, n0 = n * TN, docs = min(TM, p.count - m0), cols = min(TN, p.dim - n0);
-    GD::product({p.c + m0 * 2, p.ldc, docs * 2}, {p.x + n0 * 2, p.ldx, cols * 2}, p.rows, p.parts, p.c_part, p.x_part, lds, acc);
+    GD::product({p.c + (int64_t)m0 * SIZE, p.ldc, docs * SIZE}, {p.x + n0 * SIZE, p.ldx, cols * SIZE}, p.rows, p.parts, p.c_part, p.x_part, lds, acc);
     float f1 = p.scale, f2 = *p.most;
     if (PARTS) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(p.amax[1])); }
     const int64_t at0 = (p.first + m0) * p.ld_out + n0;
     GD::each(acc, [&](int i, int j, float v) {
         if (i >= docs || j >= cols) return;
         v = v * f1 * f2;
-        if (PARTS) __builtin_nontemporal_store(v, static_cast<float *>(p.grad_docs) + at0 + i * p.ld_out + j);
+        if (F32) __builtin_nontemporal_store(v, static_cast<float *>(p.grad_docs) + at0 + i * p.ld_out + j);
         else __builtin_nontemporal_store((__bf16)v, static_cast<__bf16 *>(p.grad_docs) + at0 + i * p.ld_out + j);
     });
 }
@@ -477,7 +499,7 @@ __global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, i
                                                  const uint32_t *__restrict__ amax, void *__restrict__ out, int64_t ld) {
     const int64_t total = (int64_t)rows * dim / 4;
     float f1 = scale, f2 = *most;
-    if (!BF16) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(amax[0])); }
+    if (amax) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(amax[0])); }
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int32_t k = 0; k < splits; k++) {
@@ -526,13 +548,29 @@ static int check_sizes(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
     return AP_OK;
 }
 
+// Up to how many queries one pass over the documents pays.
+static bool loss_few(int64_t rows, int32_t dim, int32_t dtype) { return rows <= 64 && ap_stream_lds(rows, (int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) <= AP_STREAM_LDS; }
+
+// How rows are multiplied: bf16 as they are; f32 as they are by the f32 instruction, or as two f16 parts each.  Parts cost two passes over the documents
+// and two launches more, and save most of a product's time (about 330 against 90 TFLOP/s): they pay from r queries with 8 fs r n dim above
+// 20 us + 2.6 ps n dim on (step of 100 over 2,000 of 128: 31 us in f32, 75 in parts; of 2,048 over 100,000 of 768: 9.9 and 4.1 ms).  The loss and its
+// gradient go by the same rule: a logit that is off is then off in both.
+enum LossForm { LOSS_BF16, LOSS_F32, LOSS_PARTS };
+static LossForm form_of(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
+    if (dtype == AP_BF16) return LOSS_BF16;
+    const double work = (double)n * dim;
+    if (g_ap_debug.loss_form) return g_ap_debug.loss_form == 1 ? LOSS_F32 : LOSS_PARTS;
+    return loss_few(rows, dim, dtype) || 16e-15 * rows * work < 20e-6 + 1.6e-12 * work ? LOSS_F32 : LOSS_PARTS;
+}
+
 struct LossParts {   // f32 rows as two f16 parts
-    uint32_t *amax = nullptr;
+    uint32_t *amax = nullptr, *both = nullptr;
     _Float16 *docs = nullptr, *x = nullptr;
     int64_t pad = 0, d_part = 0, x_part = 0;
     void take(LossWs &ws, int64_t rows, int64_t n, int32_t dim) {
         pad = up_to(dim, 8);
-        amax = ws.take<uint32_t>(2);
+        amax = ws.take<uint32_t>(2 * AP_LOSS_AMAX);
+        both = ws.take<uint32_t>(2);
         docs = ws.take<_Float16>(2 * n * pad);
         x = ws.take<_Float16>(2 * rows * pad);
         d_part = n * pad * 2;
@@ -540,18 +578,18 @@ struct LossParts {   // f32 rows as two f16 parts
     }
     int make(const void *xp, int64_t ldx, int64_t rows, const void *dp, int64_t ldd, int64_t n, int32_t dim, const float *coef, hipStream_t st) {
         const ApSide sd = {static_cast<const float *>(dp), ldd, n}, sx = {static_cast<const float *>(xp), ldx, rows};
-        AP_TRY(ap_fill_u32(amax, 2, 0, st));
-        hipLaunchKernelGGL(k_loss_amax, dim3((unsigned)std::min<int64_t>(div_up(n * (dim / 4), 1024), 2048)), dim3(256), 0, st, sd, sx, dim, amax);
-        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(n * (pad / 4), 256), 16384)), dim3(256), 0, st, sd, dim, (int32_t)pad, amax, nullptr, docs, docs + n * pad);
-        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)std::min<int64_t>(div_up(rows * (pad / 4), 256), 16384)), dim3(256), 0, st, sx, dim, (int32_t)pad, amax + 1, coef, x, x + rows * pad);
+        const int64_t parts = std::min<int64_t>(div_up(n * (dim / 4), 1024), AP_LOSS_AMAX);
+        const int64_t ba = std::min<int64_t>(div_up(n * (pad / 4), 256), 16384), bb = std::min<int64_t>(div_up(rows * (pad / 4), 256), 16384);
+        hipLaunchKernelGGL(k_loss_amax, dim3((unsigned)parts), dim3(256), 0, st, sd, sx, dim, amax);
+        hipLaunchKernelGGL(k_loss_split, dim3((unsigned)(ba + bb)), dim3(256), 0, st, sd, sx, (int32_t)ba, dim, (int32_t)pad, amax, (int32_t)parts, both, coef, docs, x);
         AP_CHECK_HIP(hipGetLastError());
         return AP_OK;
     }
 };
 
 // The tile that fills the compute units: the largest of 256, 128, 64 whose tiles are at least 3/4 of them.
-static int pick_tile(int64_t m, int64_t n) {
-    for (int t = 256; t > 64; t /= 2)
+static int pick_tile(int64_t m, int64_t n, LossForm form) {
+    for (int t = form == LOSS_F32 ? 128 : 256; t > 64; t /= 2)
         if (div_up(m, t) * div_up(n, t) >= 192) return t;
     return 64;
 }
@@ -562,15 +600,13 @@ static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
     AP_REQUIRE(mt * nt < (1ll << 31) / 512, "rows x n is too large");
     const dim3 grid((unsigned)(mt * nt));
     p.group = (int32_t)std::min<int64_t>(nt, 8);
-    if (tile == 256) hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
-    else if (tile == 128) hipLaunchKernelGGL((k_loss_tiles<OP, 128, 128, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
+    if (tile == 256) {
+        if constexpr (OP::BYTES == 2) hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
+    } else if (tile == 128) hipLaunchKernelGGL((k_loss_tiles<OP, 128, 128, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((k_loss_tiles<OP, 64, 64, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }
-
-// Up to how many queries one pass over the documents pays.
-static bool loss_few(int64_t rows, int32_t dim, int32_t dtype) { return rows <= 64 && ap_stream_lds(rows, (int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) <= AP_STREAM_LDS; }
 
 static int64_t few_blocks(int64_t n) { return std::min<int64_t>(div_up(n, 16 * AP_STREAM_THREADS / 64), 512); }
 
@@ -591,6 +627,7 @@ template <int DT, bool GRAD> static int launch_few(const ApLoss &p, hipStream_t 
 }
 
 struct LossPlan {
+    LossForm form;
     int tile;
     bool few;
     int64_t pairs;                 // of every query
@@ -599,12 +636,13 @@ struct LossPlan {
     LossParts parts;
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
         LossWs ws{base};
-        few = loss_few(rows, dim, dtype);
-        tile = pick_tile(n, rows);
+        form = form_of(rows, n, dim, dtype);
+        few = loss_few(rows, dim, dtype) && form != LOSS_PARTS;
+        tile = pick_tile(n, rows, form);
         pairs = few ? few_blocks(n) : div_up(n, tile);
         part = ws.take<float2>(pairs * rows);
         at_label = ws.take<float>(rows);
-        if (dtype == AP_F32 && !few) parts.take(ws, rows, n, dim);
+        if (form == LOSS_PARTS) parts.take(ws, rows, n, dim);
         return ws.bytes;
     }
 };
@@ -631,17 +669,18 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
     hipStream_t st = static_cast<hipStream_t>(stream);
     ApLoss p{};
     p.count = (int32_t)n; p.rows = (int32_t)rows; p.scale = scale; p.labels = labels; p.part = plan.part; p.at_label = plan.at_label;
+    const int64_t size = dtype == AP_BF16 ? 2 : 4;
+    p.docs = static_cast<const char *>(docs); p.x = static_cast<const char *>(x); p.ldd = ldd * size; p.ldx = ldx * size; p.dim = dim;
     if (plan.few) {
-        const int64_t size = dtype == AP_BF16 ? 2 : 4;
-        p.docs = static_cast<const char *>(docs); p.x = static_cast<const char *>(x); p.ldd = ldd * size; p.ldx = ldx * size; p.dim = dim;
         AP_TRY((dtype == AP_BF16 ? launch_few<AP_BF16, false>(p, st) : launch_few<AP_F32, false>(p, st)));
-    } else if (dtype == AP_F32) {
+    } else if (plan.form == LOSS_PARTS) {
         AP_TRY(plan.parts.make(x, ldx, rows, docs, ldd, n, dim, nullptr, st));
         p.docs = (const char *)plan.parts.docs; p.x = (const char *)plan.parts.x; p.ldd = p.ldx = plan.parts.pad * 2;
-        p.d_part = plan.parts.d_part; p.x_part = plan.parts.x_part; p.amax = plan.parts.amax; p.dim = (int32_t)plan.parts.pad;
+        p.d_part = plan.parts.d_part; p.x_part = plan.parts.x_part; p.amax = plan.parts.both; p.dim = (int32_t)plan.parts.pad;
         AP_TRY((launch_tiles<ApF16Op, true, false>(p, plan.tile, st)));
+    } else if (plan.form == LOSS_F32) {
+        AP_TRY((launch_tiles<ApF32Op, false, false>(p, plan.tile, st)));
     } else {
-        p.docs = static_cast<const char *>(docs); p.x = static_cast<const char *>(x); p.ldd = ldd * 2; p.ldx = ldx * 2; p.dim = dim;
         AP_TRY((launch_tiles<ApBf16Op, false, false>(p, plan.tile, st)));
     }
     int qb = 0;
@@ -677,6 +716,7 @@ static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k, 
 }
 
 struct GradPlan {
+    LossForm form;
     int64_t piece, ldc, c_part;
     int tile_c, tile;
     bool few, two;
@@ -685,8 +725,8 @@ struct GradPlan {
     char *c, *x;
     LossParts parts;
     // What a piece of p documents takes, in the units of pick_runs.
-    static double piece_cost(int64_t p, int64_t r, int64_t dim, int64_t parts, bool want_x) {
-        const int64_t tc = pick_tile(p, r), t = pick_tile(p, dim), more = div_up(p, t) * div_up(dim, t);
+    static double piece_cost(int64_t p, int64_t r, int64_t dim, int64_t parts, bool want_x, LossForm form) {
+        const int64_t tc = pick_tile(p, r, form), t = pick_tile(p, dim, form), more = div_up(p, t) * div_up(dim, t);
         double cost = (double)(div_up(div_up(p, tc) * div_up(r, tc), 256) * (dim * parts + 512)) * tc * tc / 65536;
         int64_t least = div_up(more, 256) * (r * parts + 512);
         if (want_x) pick_runs(div_up(r, t) * div_up(dim, t), p, more, r, parts, &least);
@@ -695,26 +735,27 @@ struct GradPlan {
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype, bool want_x) {
         LossWs ws{base};
         const int64_t r = std::max<int64_t>(rows, 1);
-        const int64_t parts = dtype == AP_F32 ? 3 : 1;
-        piece = std::min(std::max<int64_t>(AP_LOSS_PIECE_BYTES / (2 * r) / 256 * 256, 1024), up_to(n, 256));
+        form = form_of(r, n, dim, dtype);
+        const int64_t parts = form == LOSS_PARTS ? 3 : 1, size = form == LOSS_F32 ? 4 : 2;
+        piece = std::min(std::max<int64_t>(AP_LOSS_PIECE_BYTES / (size * r) / 256 * 256, 1024), up_to(n, 256));
         if (g_ap_debug.loss_piece) piece = std::min(up_to(g_ap_debug.loss_piece, 256), up_to(n, 256));
         else if (piece < n) {   // several pieces: the length of which all of them take the least time
             double least = 1e30;
             int64_t best = piece;
             for (int64_t p = piece; p >= piece / 2 && p >= 256; p -= up_to(piece / 32, 256)) {
-                const double t = (double)(n / p) * piece_cost(p, r, dim, parts, want_x) + (n % p ? piece_cost(up_to(n % p, 256), r, dim, parts, want_x) : 0);
+                const double t = (double)(n / p) * piece_cost(p, r, dim, parts, want_x, form) + (n % p ? piece_cost(up_to(n % p, 256), r, dim, parts, want_x, form) : 0);
                 if (t < least) { least = t; best = p; }
             }
             piece = best;
         }
-        ldc = piece * 2;
+        ldc = piece * size;
         // bf16 coefficients of few queries have a second part: a rounding of the label's alone would be seen in the result, and
         // where few are multiplied at once the second product costs little
         two = dtype == AP_BF16 && r <= 128;
         c_part = r * ldc;
-        few = loss_few(r, dim, dtype);
-        tile_c = pick_tile(piece, r);
-        tile = pick_tile(piece, dim);
+        few = loss_few(r, dim, dtype) && form != LOSS_PARTS;
+        tile_c = pick_tile(piece, r, form);
+        tile = pick_tile(piece, dim, form);
         if (tile > 128 && r <= 128) tile = 128;
         if (tile > 64 && r <= 64) tile = 64;
         runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts);
@@ -722,10 +763,10 @@ struct GradPlan {
         runs = (int32_t)div_up(piece, run_docs);
         most = ws.take<float>(1);
         coef = ws.take<float>(r);
-        c = ws.take<char>(c_part * (dtype == AP_F32 || two ? 2 : 1));
+        c = ws.take<char>(c_part * (form == LOSS_PARTS || two ? 2 : 1));
         gx = want_x ? ws.take<float>(runs * r * dim) : nullptr;
-        if (dtype == AP_F32) this->parts.take(ws, r, n, dim);
-        else x = ws.take<char>(r * dim * 2);
+        if (form == LOSS_PARTS) this->parts.take(ws, r, n, dim);
+        else x = ws.take<char>(r * dim * size);
         return ws.bytes;
     }
 };
@@ -746,7 +787,7 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, const ApLoss &few, ApLoss
         if (plan.few) {
             ApLoss f = p;
             f.docs = few.docs; f.x = few.x; f.ldd = few.ldd; f.ldx = few.ldx; f.dim = few.dim;
-            AP_TRY((launch_few<PARTS ? AP_F32 : AP_BF16, true>(f, st)));
+            AP_TRY((launch_few<OP::BYTES == 4 ? AP_F32 : AP_BF16, true>(f, st)));
         } else {
             AP_TRY((launch_tiles<OP, PARTS, true>(p, plan.tile_c, st)));
         }
@@ -756,8 +797,9 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, const ApLoss &few, ApLoss
         // a short last piece leaves the runs past its end alone
         g.runs = (uint32_t)(!g.gx ? 0 : g.start ? plan.runs : div_up(g.count, plan.run_docs));
         const dim3 grid((unsigned)(g.runs * div_up(g.rows, plan.tile) * nt + (g.grad_docs ? div_up(g.count, plan.tile) * nt : 0)));
-        if (plan.tile == 256) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
-        else if (plan.tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        if (plan.tile == 256) {
+            if constexpr (OP::BYTES == 2) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
+        } else if (plan.tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         else hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         AP_CHECK_HIP(hipGetLastError());
     }
@@ -778,31 +820,41 @@ extern "C" int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, co
     GradPlan plan;
     const size_t need = plan.lay(static_cast<char *>(workspace), rows, n, dim, dtype, grad_x != nullptr);
     AP_REQUIRE(workspace && bytes >= need, "workspace of %zu bytes, %zu are needed", bytes, need);
-    hipLaunchKernelGGL(k_loss_most, dim3(1), dim3(1024), 0, st, row_grad, labels, (int32_t)rows, (int32_t)n, plan.most, plan.coef);
+    const bool parts = plan.form == LOSS_PARTS;
+    const int64_t size = dtype == AP_BF16 ? 2 : 4;
+    const int32_t groups = (int32_t)(dim * size / 16);
+    const float *given = nullptr;
+    uint4 *used = parts ? nullptr : reinterpret_cast<uint4 *>(plan.x);
+    if (rows > AP_LOSS_PREP) {
+        hipLaunchKernelGGL(k_loss_prep, dim3(1), dim3(1024), 0, st, row_grad, labels, (int32_t)rows, (int32_t)n, nullptr, plan.most, nullptr, nullptr, 0, 0, nullptr);
+        given = plan.most;
+    }
+    hipLaunchKernelGGL(k_loss_prep, dim3((unsigned)std::min<int64_t>(div_up(used ? rows * groups : rows, 1024), 512)), dim3(1024), 0, st, row_grad, labels, (int32_t)rows, (int32_t)n, given,
+                       plan.most, plan.coef, static_cast<const char *>(x), ldx * size, groups, used);
+    AP_CHECK_HIP(hipGetLastError());
     ApLoss p{};
     ApLossGrad g{};
     p.rows = g.rows = (int32_t)rows;
     p.scale = g.scale = scale;
-    p.labels = labels; p.lse = lse; p.coef = plan.coef; p.c = plan.c; p.ldc = g.ldc = plan.ldc; p.c_part = g.c_part = dtype == AP_F32 || plan.two ? plan.c_part : 0;
-    g.parts = dtype == AP_F32 ? 3 : plan.two ? 2 : 1;
+    p.labels = labels; p.lse = lse; p.coef = plan.coef; p.c = plan.c; p.ldc = g.ldc = plan.ldc; p.c_part = g.c_part = parts || plan.two ? plan.c_part : 0;
+    g.parts = parts ? 3 : plan.two ? 2 : 1;
     g.c = plan.c; g.most = plan.most; g.grad_docs = grad_docs; g.ld_out = dim; g.gx = plan.gx; g.dim = dim;
     ApLoss few = p;   // the rows as they are
-    const int64_t size = dtype == AP_BF16 ? 2 : 4;
     few.docs = static_cast<const char *>(docs); few.x = static_cast<const char *>(x); few.ldd = ldd * size; few.ldx = ldx * size; few.dim = dim;
     const unsigned join = (unsigned)std::min<int64_t>(div_up(rows * dim / 4, 256), 4096);
-    if (dtype == AP_F32) {
+    if (parts) {
         const LossParts &q = plan.parts;
         AP_TRY(plan.parts.make(x, ldx, rows, docs, ldd, n, dim, plan.coef, st));
         p.docs = g.docs = (const char *)q.docs; p.x = g.x = (const char *)q.x; p.ldd = p.ldx = g.ldd = g.ldx = q.pad * 2;
-        p.d_part = g.d_part = q.d_part; p.x_part = g.x_part = q.x_part; p.amax = g.amax = q.amax; p.dim = (int32_t)q.pad;
+        p.d_part = g.d_part = q.d_part; p.x_part = g.x_part = q.x_part; p.amax = g.amax = q.both; p.dim = (int32_t)q.pad;
         AP_TRY((loss_pieces<ApF16Op, true>(plan, p, few, g, n, st)));
-        if (grad_x) hipLaunchKernelGGL((k_loss_gx<false>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, q.amax, grad_x, (int64_t)dim);
     } else {
-        hipLaunchKernelGGL(k_loss_used, dim3((unsigned)std::min<int64_t>(div_up(rows * dim / 8, 256), 4096)), dim3(256), 0, st, static_cast<const char *>(x), ldx * 2, (int32_t)rows,
-                           dim / 8, plan.coef, reinterpret_cast<uint4 *>(plan.x));
-        p.docs = g.docs = static_cast<const char *>(docs); p.x = g.x = plan.x; p.ldd = g.ldd = ldd * 2; p.ldx = g.ldx = (int64_t)dim * 2; p.dim = dim;
-        AP_TRY((loss_pieces<ApBf16Op, false>(plan, p, few, g, n, st)));
-        if (grad_x) hipLaunchKernelGGL((k_loss_gx<true>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, nullptr, grad_x, (int64_t)dim);
+        p.docs = g.docs = static_cast<const char *>(docs); p.x = g.x = plan.x; p.ldd = g.ldd = ldd * size; p.ldx = g.ldx = dim * size; p.dim = dim;
+        AP_TRY((dtype == AP_BF16 ? loss_pieces<ApBf16Op, false>(plan, p, few, g, n, st) : loss_pieces<ApF32Op, false>(plan, p, few, g, n, st)));
+    }
+    if (grad_x) {
+        if (dtype == AP_BF16) hipLaunchKernelGGL((k_loss_gx<true>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, nullptr, grad_x, (int64_t)dim);
+        else hipLaunchKernelGGL((k_loss_gx<false>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, g.amax, grad_x, (int64_t)dim);
     }
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
