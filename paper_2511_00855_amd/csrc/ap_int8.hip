@@ -191,7 +191,7 @@ extern "C" int ap_scores_int8_bytes(int64_t rows, int32_t dim, int32_t x_dtype, 
 template <int DT> static int few(const ApScores8 &p, hipStream_t st) {
     const int nq = (p.rows + 15) / 16;
     const size_t lds = (size_t)ap_stream_lds(p.rows, p.pad);
-    const dim3 grid((unsigned)std::min<int64_t>(div_up(div_up(p.n, 16), AP_STREAM_THREADS / 64), 512));
+    const dim3 grid((unsigned)ap_stream_blocks(p.n));
 #define AP_FEW(N)                                                                                                                       \
     case N:                                                                                                                             \
         if (lds > 60 * 1024) AP_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_scores8_few<DT, N>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \

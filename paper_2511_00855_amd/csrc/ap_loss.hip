@@ -117,6 +117,8 @@ struct ApLoss {
     int64_t ldc, c_part;           // in bytes; c_part 0: coefficients of one part
 };
 
+#define AP_LOSS_PIECE_BYTES ((int64_t)128 << 20)   // of the coefficients of a piece, one part: they stay in the last cache until they are multiplied
+
 // What a product becomes a logit times log2(e) by: two factors, each of which is a number where their product may not be.  Maxima and the label's
 // product are kept as they are and only differences are multiplied (the factors are positive): a loss much smaller than its logits keeps
 // its bits.
@@ -350,8 +352,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
             const int64_t d = first + (lane >> 4) * 4;
 #pragma unroll
             for (int g = 0; g < NQ; g++) {
-                const int q = g * 16 + (lane & 15);
-                if (q >= p.rows) continue;
+                const int q = g * 16 + (lane & 15);   // past the last query: weight 0
                 const ApCoef co(coef[g], lse[g]);
                 float v[4];
 #pragma unroll
@@ -359,13 +360,9 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
                     const float e = co.exp_of(f.of<false>(acc[g][r])) - (label[g] == p.first + d + r ? 1.f : 0.f);
                     v[r] = d + r < p.count ? co.times(e) : 0.f;
                 }
-                char *to = p.c + q * p.ldc + d * SIZE;
-                if constexpr (DT == AP_F32) {
-                    *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
-                } else {
-                    *reinterpret_cast<uint2 *>(to) = ap_coef_part<false>(v);
-                    if (p.c_part) *reinterpret_cast<uint2 *>(to + p.c_part) = ap_coef_part<false>(v);
-                }
+                float *to = reinterpret_cast<float *>(p.c) + d * (NQ * 16) + q;   // [document][query]
+#pragma unroll
+                for (int r = 0; r < 4; r++) to[r * (NQ * 16)] = v[r];
             }
         });
         return;
@@ -494,6 +491,28 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
     });
 }
 
+// The sums of many runs: 16 threads share an element's.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_loss_gx_many(const float *__restrict__ gx, int32_t runs, int64_t total, float scale, const float *__restrict__ most, void *__restrict__ out) {
+    __shared__ float4 s_sum[16][16];
+    const int l = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t i = blockIdx.x * (int64_t)16 + l;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < total)
+#pragma unroll 8
+        for (int32_t k = part; k < runs; k += 16) {
+            const float4 v = reinterpret_cast<const float4 *>(gx)[k * total + i];
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+    s_sum[part][l] = s;
+    __syncthreads();
+    if (part || i >= total) return;
+    for (int k = 1; k < 16; k++) { const float4 v = s_sum[k][l]; s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w; }
+    const float f1 = scale, f2 = *most;
+    s.x = s.x * f1 * f2; s.y = s.y * f1 * f2; s.z = s.z * f1 * f2; s.w = s.w * f1 * f2;
+    if (BF16) reinterpret_cast<uint2 *>(out)[i] = make_uint2(ap_bf16_pair(s.x, s.y), ap_bf16_pair(s.z, s.w));
+    else reinterpret_cast<float4 *>(out)[i] = s;
+}
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, int32_t splits, int32_t rows, int32_t dim, float scale, const float *__restrict__ most,
                                                  const uint32_t *__restrict__ amax, void *__restrict__ out, int64_t ld) {
@@ -511,6 +530,145 @@ __global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, i
         if (BF16) *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + r * ld + c) = make_uint2(ap_bf16_pair(s.x, s.y), ap_bf16_pair(s.z, s.w));
         else *reinterpret_cast<float4 *>(static_cast<float *>(out) + r * ld + c) = s;
     }
+}
+
+// Few queries: both gradients in one pass over the documents, which reads and writes every row once; f32 products whatever the type.  A wave
+// has NB blocks of 16 columns: VEC values of a lane's load belong to as many blocks, so that block t is made of the columns VEC n + t and
+// loads and stores are whole lines.  16 documents at a time: their rows times the coefficients go to sums of the queries' gradient that stay
+// in registers, the queries (in registers too) times the coefficients are the documents' gradient.
+struct ApLossFew {
+    const char *docs, *x;          // x: without queries of weight 0
+    int64_t ldd, ldx;
+    const float *c;                // [document of the piece][query]
+    int64_t first;
+    int32_t count, rows, dim;
+    float scale;
+    const float *most;
+    void *grad_docs;               // NULL: not wanted
+    float *gx;                     // NULL: not wanted; [workgroup][query][dim], sums so far
+    int32_t start, tiles;          // tiles of 16 documents of a workgroup
+};
+template <int DT, int NQ, int NB>
+__global__ __launch_bounds__(512) void k_loss_few_grads(ApLossFew p) {
+    constexpr int SIZE = DT == AP_F32 ? 4 : 2, VEC = DT == AP_F32 ? 4 : NB == 8 ? 8 : 4, GROUPS = NB / VEC, WORDS = VEC * SIZE / 4;
+    const int lane = threadIdx.x & 63, n = lane & 15, k4 = lane >> 4;
+    const int col0 = (blockIdx.y * 8 + ap_wave_id()) * (NB * 16) + n * VEC;   // of group g: col0 + 16 VEC g
+    if ((blockIdx.y * 8 + ap_wave_id()) * (NB * 16) >= p.dim) return;
+    auto load = [&](const char *at, uint32_t (&w)[WORDS]) {
+        if constexpr (WORDS == 4) { const uint4 v = *reinterpret_cast<const uint4 *>(at); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+        else { const uint2 v = *reinterpret_cast<const uint2 *>(at); w[0] = v.x; w[1] = v.y; }
+    };
+    auto value = [&](const uint32_t (&w)[WORDS], int t) -> float {
+        if constexpr (DT == AP_F32) return __uint_as_float(w[t]);
+        else return __uint_as_float(t & 1 ? w[t / 2] & 0xffff0000u : w[t / 2] << 16);
+    };
+    // the queries: step i of group q takes query 16 q + 4 (lane / 16) + i
+    float x[NQ][4][NB];
+    ap_s_f32x4 sum[NQ][NB];
+#pragma unroll
+    for (int q = 0; q < NQ; q++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int row = q * 16 + k4 * 4 + i;
+#pragma unroll
+            for (int g = 0; g < GROUPS; g++) {
+                const int col = col0 + g * 16 * VEC;
+                uint32_t w[WORDS];
+#pragma unroll
+                for (int j = 0; j < WORDS; j++) w[j] = 0;
+                if (p.grad_docs && row < p.rows && col < p.dim) load(p.x + row * p.ldx + col * SIZE, w);
+#pragma unroll
+                for (int t = 0; t < VEC; t++) x[q][i][g * VEC + t] = value(w, t);
+            }
+        }
+#pragma unroll
+    for (int q = 0; q < NQ; q++)
+#pragma unroll
+        for (int b = 0; b < NB; b++) sum[q][b] = ap_s_f32x4{0.f, 0.f, 0.f, 0.f};
+    const float f1 = p.scale, f2 = *p.most;
+    const int64_t d0 = (int64_t)blockIdx.x * p.tiles * 16, end = min(d0 + p.tiles * 16, (int64_t)(p.count + 15) / 16 * 16);
+    uint32_t w[4][GROUPS][WORDS];
+    float cx[NQ][4], cd[NQ][4];
+    // document j + 4 i + lane / 16 for the queries' gradient, coefficients of document j + lane % 16 for the documents'
+    auto bring = [&](int64_t j) {
+#pragma unroll
+        for (int q = 0; q < NQ; q++) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) cx[q][i] = p.c[(j + i * 4 + k4) * (NQ * 16) + q * 16 + n];
+            const float4 v = *reinterpret_cast<const float4 *>(p.c + (j + n) * (NQ * 16) + q * 16 + k4 * 4);
+            cd[q][0] = v.x; cd[q][1] = v.y; cd[q][2] = v.z; cd[q][3] = v.w;
+        }
+        if (p.gx)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int64_t d = min(j + i * 4 + k4, (int64_t)p.count - 1);   // past the end: the last row, of coefficient 0
+#pragma unroll
+                for (int g = 0; g < GROUPS; g++) {
+                    const int col = col0 + g * 16 * VEC;
+                    load(p.docs + (p.first + d) * p.ldd + (col < p.dim ? col : 0) * SIZE, w[i][g]);
+                }
+            }
+    };
+    for (int64_t j = d0; j < end; j += 16) {
+        bring(j);
+        if (p.grad_docs) {
+            ap_s_f32x4 out[NB];
+#pragma unroll
+            for (int b = 0; b < NB; b++) {
+                out[b] = ap_s_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int q = 0; q < NQ; q++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) out[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(cd[q][i], x[q][i][b], out[b], 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                const int64_t d = j + k4 * 4 + r;
+                if (d >= p.count) continue;
+#pragma unroll
+                for (int g = 0; g < GROUPS; g++) {
+                    const int col = col0 + g * 16 * VEC;
+                    if (col >= p.dim) continue;
+                    char *to = static_cast<char *>(p.grad_docs) + ((p.first + d) * p.dim + col) * SIZE;
+                    float v[VEC];
+#pragma unroll
+                    for (int t = 0; t < VEC; t++) v[t] = out[g * VEC + t][r] * f1 * f2;
+                    typedef uint32_t words __attribute__((ext_vector_type(WORDS)));
+                    words u;
+#pragma unroll
+                    for (int k = 0; k < WORDS; k++) u[k] = DT == AP_F32 ? __float_as_uint(v[k]) : ap_bf16_pair(v[(2 * k) % VEC], v[(2 * k + 1) % VEC]);
+                    __builtin_nontemporal_store(u, reinterpret_cast<words *>(to));
+                }
+            }
+        }
+        if (p.gx)
+#pragma unroll
+            for (int q = 0; q < NQ; q++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int b = 0; b < NB; b++) sum[q][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(cx[q][i], value(w[i][b / VEC], b % VEC), sum[q][b], 0, 0, 0);
+    }
+    if (!p.gx) return;
+#pragma unroll
+    for (int q = 0; q < NQ; q++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int row = q * 16 + k4 * 4 + r;
+            if (row >= p.rows) continue;
+#pragma unroll
+            for (int g = 0; g < GROUPS; g++) {
+                const int col = col0 + g * 16 * VEC;
+                if (col >= p.dim) continue;
+                float *to = p.gx + ((int64_t)blockIdx.x * p.rows + row) * p.dim + col;
+#pragma unroll
+                for (int t = 0; t < VEC; t += 4) {
+                    float4 v = make_float4(sum[q][g * VEC + t][r], sum[q][g * VEC + t + 1][r], sum[q][g * VEC + t + 2][r], sum[q][g * VEC + t + 3][r]);
+                    if (!p.start) { const float4 o = *reinterpret_cast<const float4 *>(to + t); v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
+                    *reinterpret_cast<float4 *>(to + t) = v;
+                }
+            }
+        }
 }
 
 // ------------------------------------------------------------------ host side
@@ -608,12 +766,10 @@ static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
     return AP_OK;
 }
 
-static int64_t few_blocks(int64_t n) { return std::min<int64_t>(div_up(n, 16 * AP_STREAM_THREADS / 64), 512); }
-
 template <int DT, bool GRAD> static int launch_few(const ApLoss &p, hipStream_t st) {
     // the pairs of the waves take the queries' place
     const size_t lds = (size_t)std::max<int64_t>(ap_stream_lds(p.rows, (int64_t)p.dim * (DT == AP_F32 ? 4 : 2)), div_up(p.rows, 16) * 16 * 8 * (AP_STREAM_THREADS / 64));
-    const int64_t blocks = few_blocks(p.count);
+    const int64_t blocks = ap_stream_blocks(p.count);
     const dim3 grid((unsigned)blocks);
 #define AP_FEW(N)                                                                                                                       \
     case N:                                                                                                                             \
@@ -639,7 +795,7 @@ struct LossPlan {
         form = form_of(rows, n, dim, dtype);
         few = loss_few(rows, dim, dtype) && form != LOSS_PARTS;
         tile = pick_tile(n, rows, form);
-        pairs = few ? few_blocks(n) : div_up(n, tile);
+        pairs = few ? ap_stream_blocks(n) : div_up(n, tile);
         part = ws.take<float2>(pairs * rows);
         at_label = ws.take<float>(rows);
         if (form == LOSS_PARTS) parts.take(ws, rows, n, dim);
@@ -691,7 +847,6 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
     return AP_OK;
 }
 
-#define AP_LOSS_PIECE_BYTES ((int64_t)128 << 20)   // of the coefficients of a piece, one part: they stay in the last cache until they are multiplied
 
 // In how many runs of its documents the queries' gradient is made, so that its workgroups (`tiles` a run, taken first) and the `more` of the documents'
 // gradient, `k` long, end together on 256 compute units.  A workgroup costs its length and about 512 for its start and end.
@@ -737,6 +892,20 @@ struct GradPlan {
         const int64_t r = std::max<int64_t>(rows, 1);
         form = form_of(r, n, dim, dtype);
         const int64_t parts = form == LOSS_PARTS ? 3 : 1, size = form == LOSS_F32 ? 4 : 2;
+        few = loss_few(r, dim, dtype) && form != LOSS_PARTS;
+        if (few) {   // workgroups of a whole number of 16 documents, as many as there are compute units
+            const int64_t r16 = up_to(r, 16);
+            piece = std::min<int64_t>(AP_LOSS_PIECE_BYTES / (r16 * 4) / 256 * 256, up_to(n, 16));
+            if (g_ap_debug.loss_piece) piece = std::min(up_to(g_ap_debug.loss_piece, 256), up_to(n, 16));
+            run_docs = (int32_t)div_up(piece / 16, 256);   // in tiles
+            runs = (int32_t)div_up(piece / 16, run_docs);
+            most = ws.take<float>(1);
+            coef = ws.take<float>(r);
+            c = ws.take<char>(piece * r16 * 4);
+            gx = want_x ? ws.take<float>(runs * r * dim) : nullptr;
+            x = ws.take<char>(r * dim * (dtype == AP_BF16 ? 2 : 4));
+            return ws.bytes;
+        }
         piece = std::min(std::max<int64_t>(AP_LOSS_PIECE_BYTES / (size * r) / 256 * 256, 1024), up_to(n, 256));
         if (g_ap_debug.loss_piece) piece = std::min(up_to(g_ap_debug.loss_piece, 256), up_to(n, 256));
         else if (piece < n) {   // several pieces: the length of which all of them take the least time
@@ -753,7 +922,6 @@ struct GradPlan {
         // where few are multiplied at once the second product costs little
         two = dtype == AP_BF16 && r <= 128;
         c_part = r * ldc;
-        few = loss_few(r, dim, dtype) && form != LOSS_PARTS;
         tile_c = pick_tile(piece, r, form);
         tile = pick_tile(piece, dim, form);
         if (tile > 128 && r <= 128) tile = 128;
@@ -780,17 +948,11 @@ extern "C" int ap_softmax_loss_grad_bytes(int64_t rows, int64_t n, int32_t dim, 
 }
 
 template <class OP, bool PARTS>
-static int loss_pieces(const GradPlan &plan, ApLoss p, const ApLoss &few, ApLossGrad g, int64_t n, hipStream_t st) {
+static int loss_pieces(const GradPlan &plan, ApLoss p, ApLossGrad g, int64_t n, hipStream_t st) {
     for (int64_t d0 = 0; d0 < n; d0 += plan.piece) {
         p.first = g.first = d0;
         p.count = g.count = (int32_t)std::min(plan.piece, n - d0);
-        if (plan.few) {
-            ApLoss f = p;
-            f.docs = few.docs; f.x = few.x; f.ldd = few.ldd; f.ldx = few.ldx; f.dim = few.dim;
-            AP_TRY((launch_few<OP::BYTES == 4 ? AP_F32 : AP_BF16, true>(f, st)));
-        } else {
-            AP_TRY((launch_tiles<OP, PARTS, true>(p, plan.tile_c, st)));
-        }
+        AP_TRY((launch_tiles<OP, PARTS, true>(p, plan.tile_c, st)));
         const int64_t nt = div_up(g.dim, plan.tile);
         g.run_docs = plan.run_docs;
         g.start = d0 == 0;
@@ -801,6 +963,27 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, const ApLoss &few, ApLoss
             if constexpr (OP::BYTES == 2) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
         } else if (plan.tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         else hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        AP_CHECK_HIP(hipGetLastError());
+    }
+    return AP_OK;
+}
+
+template <int DT>
+static int few_pieces(const GradPlan &plan, ApLoss p, ApLossFew f, int64_t n, hipStream_t st) {
+    for (int64_t d0 = 0; d0 < n; d0 += plan.piece) {
+        p.first = f.first = d0;
+        p.count = f.count = (int32_t)std::min(plan.piece, n - d0);
+        AP_TRY((launch_few<DT, true>(p, st)));
+        f.tiles = plan.run_docs;
+        f.start = d0 == 0;
+        // a short last piece leaves the sums of the workgroups past its end alone
+        const unsigned blocks = (unsigned)(f.start ? plan.runs : div_up(div_up(f.count, 16), plan.run_docs));
+        const int nq = (f.rows + 15) / 16, nb = nq <= 2 ? 8 : 4;
+        const dim3 grid(blocks, (unsigned)div_up(f.dim, 8 * nb * 16));
+        if (nq == 1) hipLaunchKernelGGL((k_loss_few_grads<DT, 1, 8>), grid, dim3(512), 0, st, f);
+        else if (nq == 2) hipLaunchKernelGGL((k_loss_few_grads<DT, 2, 8>), grid, dim3(512), 0, st, f);
+        else if (nq == 3) hipLaunchKernelGGL((k_loss_few_grads<DT, 3, 4>), grid, dim3(512), 0, st, f);
+        else hipLaunchKernelGGL((k_loss_few_grads<DT, 4, 4>), grid, dim3(512), 0, st, f);
         AP_CHECK_HIP(hipGetLastError());
     }
     return AP_OK;
@@ -839,18 +1022,27 @@ extern "C" int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, co
     p.labels = labels; p.lse = lse; p.coef = plan.coef; p.c = plan.c; p.ldc = g.ldc = plan.ldc; p.c_part = g.c_part = parts || plan.two ? plan.c_part : 0;
     g.parts = parts ? 3 : plan.two ? 2 : 1;
     g.c = plan.c; g.most = plan.most; g.grad_docs = grad_docs; g.ld_out = dim; g.gx = plan.gx; g.dim = dim;
-    ApLoss few = p;   // the rows as they are
-    few.docs = static_cast<const char *>(docs); few.x = static_cast<const char *>(x); few.ldd = ldd * size; few.ldx = ldx * size; few.dim = dim;
+    if (plan.few) {
+        ApLoss q = p;
+        q.docs = static_cast<const char *>(docs); q.x = static_cast<const char *>(x); q.ldd = ldd * size; q.ldx = ldx * size; q.dim = dim;
+        const ApLossFew f{q.docs, plan.x, q.ldd, dim * size, reinterpret_cast<const float *>(plan.c), 0, 0, (int32_t)rows, dim, scale, plan.most, grad_docs, plan.gx, 0, 0};
+        AP_TRY((dtype == AP_BF16 ? few_pieces<AP_BF16>(plan, q, f, n, st) : few_pieces<AP_F32>(plan, q, f, n, st)));
+        const int64_t total = rows * dim / 4;
+        if (grad_x && dtype == AP_BF16) hipLaunchKernelGGL((k_loss_gx_many<true>), dim3((unsigned)div_up(total, 16)), dim3(256), 0, st, plan.gx, plan.runs, total, scale, plan.most, grad_x);
+        else if (grad_x) hipLaunchKernelGGL((k_loss_gx_many<false>), dim3((unsigned)div_up(total, 16)), dim3(256), 0, st, plan.gx, plan.runs, total, scale, plan.most, grad_x);
+        AP_CHECK_HIP(hipGetLastError());
+        return AP_OK;
+    }
     const unsigned join = (unsigned)std::min<int64_t>(div_up(rows * dim / 4, 256), 4096);
     if (parts) {
         const LossParts &q = plan.parts;
         AP_TRY(plan.parts.make(x, ldx, rows, docs, ldd, n, dim, plan.coef, st));
         p.docs = g.docs = (const char *)q.docs; p.x = g.x = (const char *)q.x; p.ldd = p.ldx = g.ldd = g.ldx = q.pad * 2;
         p.d_part = g.d_part = q.d_part; p.x_part = g.x_part = q.x_part; p.amax = g.amax = q.both; p.dim = (int32_t)q.pad;
-        AP_TRY((loss_pieces<ApF16Op, true>(plan, p, few, g, n, st)));
+        AP_TRY((loss_pieces<ApF16Op, true>(plan, p, g, n, st)));
     } else {
         p.docs = g.docs = static_cast<const char *>(docs); p.x = g.x = plan.x; p.ldd = g.ldd = ldd * size; p.ldx = g.ldx = dim * size; p.dim = dim;
-        AP_TRY((dtype == AP_BF16 ? loss_pieces<ApBf16Op, false>(plan, p, few, g, n, st) : loss_pieces<ApF32Op, false>(plan, p, few, g, n, st)));
+        AP_TRY((dtype == AP_BF16 ? loss_pieces<ApBf16Op, false>(plan, p, g, n, st) : loss_pieces<ApF32Op, false>(plan, p, g, n, st)));
     }
     if (grad_x) {
         if (dtype == AP_BF16) hipLaunchKernelGGL((k_loss_gx<true>), dim3(join), dim3(256), 0, st, plan.gx, plan.runs, (int32_t)rows, dim, scale, plan.most, nullptr, grad_x, (int64_t)dim);
