@@ -467,6 +467,7 @@ int ap_search_form(const ap_index *index, int32_t out3[3]);
  *   "search_floor"            1: no neighbour waits below the estimated end of the pool, 2: the estimate is far too high
  *   "loss_piece"              documents whose coefficients the gradient of the softmax loss holds at a time
  *   "loss_form"               1: the softmax loss multiplies f32 rows by the f32 instruction, 2: as two f16 parts (rounded otherwise)
+ *   "loss_few"                one more than the number of queries (at most 64) that the softmax loss takes in passes over the documents
  *   "embed_few"               one more than the number of entries up to which the embedding's gradient sorts nothing
  *   "search_visited_global"   1: visited sets stay in the global workspace even where the search would keep them in LDS
  *   "search_query_lists"      1: the plain and keyword searches look query terms up in the query's lists, not in LDS tables

@@ -155,7 +155,7 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
 
     // The whole product of K values.  With `parts` > 1 the operands are sums of parts that lie `a_part` / `b_part` bytes apart and the
     // product takes `parts` = 3 pairs: second times first, first times second, first times first (the smallest first; the product
-    // of the second parts is below the last bit of the sum).
+    // of the second parts is below the last bit of the sum).  2: only one operand has a second part, and the other's `.._part` is 0.
     static __device__ __forceinline__ void product(const ApOperand &A, const ApOperand &B, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB]) {
         const int lane = threadIdx.x & 63, wave = ap_wave_id();
         const int wm = wave / WN, wn = wave % WN;
@@ -190,24 +190,19 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
             load<TN, B_LINE>(b, ob, B_LINE ? left * OP::BYTES : left, lds0 + stage * STAGE + A_BYTES, wave, lane);
             advance();
         };
-        // A step's fragments are read while the step before is multiplied.  The barrier stands before the last step of a chunk: every wave has the
-        // chunk's last fragments in registers then, so its stage is filled again, and the next chunk has come.  The order is laid down
-        // (the compiler would put all reads before or behind the multiplications) and nothing in a chunk branches.
-        ap_g_i32x4 fr[2][FB + FA];
-        constexpr int NR = FA + FB, NM = FA * FB;
-        auto read1 = [&](int stage, int s, int to, int i) {
-            const char *sa = lds + stage * STAGE, *sb = sa + A_BYTES;
-            if (i < FB) fr[to][i] = frag<TN, B_LINE>(sb, wn * (TN / WN) + i * 16, s, lane);
-            else fr[to][i] = frag<TM, A_LINE>(sa, wm * (TM / WM) + (i - FB) * 16, s, lane);
-        };
-        auto mul = [&](int from, auto between) {
-#pragma unroll
-            for (int i = 0; i < NM; i++) {
-                between(i);
-                __builtin_amdgcn_sched_barrier(0);
-                acc[i / FB][i % FB] = OP::mul(fr[from][FB + i / FB], fr[from][i % FB], acc[i / FB][i % FB]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        // A step's fragments are read while the step before is multiplied: B's into the other of two sets, A's each into its own place when the last block
+        // that needs it has been issued (a second set of A's would leave too few registers, and what the compiler then keeps in memory waits
+        // for the loads).  The barrier stands in a chunk's last step, behind the first blocks: every wave has the chunk's last fragments in
+        // registers then, so its stage is filled again, and the next chunk has come.  The order is laid down (the compiler would put all reads
+        // before or behind the multiplications) and nothing in a chunk branches.
+        ap_g_i32x4 fa[FA], fb[2][FB];
+        constexpr int NM = FA * FB, MEET = FA / 4 * FB;
+        auto read_a = [&](int stage, int s, int a) { fa[a] = frag<TM, A_LINE>(lds + stage * STAGE, wm * (TM / WM) + a * 16, s, lane); };
+        auto read_b = [&](int stage, int s, int b) { fb[s][b] = frag<TN, B_LINE>(lds + stage * STAGE + A_BYTES, wn * (TN / WN) + b * 16, s, lane); };
+        auto mul = [&](int s, int i) {
+            __builtin_amdgcn_sched_barrier(0);
+            acc[i / FB][i % FB] = OP::mul(fa[i / FB], fb[s][i % FB], acc[i / FB][i % FB]);
+            __builtin_amdgcn_sched_barrier(0);
         };
         if (chunks > 0) {
             bring(0);
@@ -215,7 +210,9 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
             ap_g_barrier();
             if (chunks > 1) bring(1);
 #pragma unroll
-            for (int i = 0; i < NR; i++) read1(0, 0, 0, i);
+            for (int b = 0; b < FB; b++) read_b(0, 0, b);
+#pragma unroll
+            for (int a = 0; a < FA; a++) read_a(0, 0, a);
         }
         // f32 products add four values of k at a time: sums of 256 are added up apart, or a long sum would be off by the root of its length
         Acc total[OP::BYTES == 4 ? FA : 1][OP::BYTES == 4 ? FB : 1];
@@ -224,25 +221,33 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
             for (int i = 0; i < NM; i++) total[i / FB][i % FB] = Acc{0, 0, 0, 0};
         for (int32_t c = 0; c < chunks; c++) {
             const int st = c & 1;
-            mul(0, [&](int i) {   // the reads in the first half
 #pragma unroll
-                for (int r = min(NR, i * NR * 2 / NM); r < min(NR, (i + 1) * NR * 2 / NM); r++) read1(st, 1, 1, r);
-            });
+            for (int i = 0; i < NM; i++) {
+                if (i < FB) read_b(st, 1, i);
+                mul(0, i);
+                if (i % FB == FB - 1) read_a(st, 1, i / FB);
+            }
+#pragma unroll
+            for (int i = 0; i < MEET; i++) mul(1, i);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             ap_g_wait_loads<0>();
             ap_g_barrier();
             // past the last chunk nothing is left: the loads bring zeros that nobody reads
             const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
             const int32_t la = ap_uniform_i32(A_LINE ? left * OP::BYTES : left), lb = ap_uniform_i32(B_LINE ? left * OP::BYTES : left);
-            mul(1, [&](int i) {
 #pragma unroll
-                for (int r = min(NR, i * NR * 2 / NM); r < min(NR, (i + 1) * NR * 2 / NM); r++) read1(st ^ 1, 0, 0, r);
+            for (int i = MEET; i < NM; i++) {
+                const int k = i - MEET, n = NM - MEET;
+                if (k < FB) read_b(st ^ 1, 0, k);
+                if (k < MEET / FB) read_a(st ^ 1, 0, k);
 #pragma unroll
-                for (int l = i * (LA + LB) / NM; l < (i + 1) * (LA + LB) / NM; l++) {
+                for (int l = k * (LA + LB) / n; l < (k + 1) * (LA + LB) / n; l++) {
                     if (l < LA) load1<TM, A_LINE>(a, oa, la, lds0 + st * STAGE, wave, lane, l);
                     else load1<TN, B_LINE>(b, ob, lb, lds0 + st * STAGE + A_BYTES, wave, lane, l - LA);
                 }
-            });
+                mul(1, i);
+                if (i % FB == FB - 1) read_a(st ^ 1, 0, i / FB);
+            }
             advance();
             if constexpr (OP::BYTES == 4)
                 if ((c & 7) == 7 || c + 1 == chunks)

@@ -110,6 +110,7 @@ struct ApLoss {
     float scale;
     const int32_t *labels;
     int32_t group;                 // column tiles that an XCD's workgroups take together
+    int32_t all;                   // few queries: how many there are in all groups; `rows` of them are this one's
     float2 *part;                  // loss: [row tile][query] maximum, sum
     float *at_label;               // loss: the label's product
     const float *lse, *coef;       // gradient: of each query; g_q over the largest, 0 where it has no label
@@ -360,9 +361,10 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
                     const float e = co.exp_of(f.of<false>(acc[g][r])) - (label[g] == p.first + d + r ? 1.f : 0.f);
                     v[r] = d + r < p.count ? co.times(e) : 0.f;
                 }
-                float *to = reinterpret_cast<float *>(p.c) + d * (NQ * 16) + q;   // [document][query]
+                const int all = (p.all + 15) / 16 * 16;
+                float *to = reinterpret_cast<float *>(p.c) + d * all + q;   // [document][query]
 #pragma unroll
-                for (int r = 0; r < 4; r++) to[r * (NQ * 16)] = v[r];
+                for (int r = 0; r < 4; r++) to[r * all] = v[r];
             }
         });
         return;
@@ -398,7 +400,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
     for (int q = threadIdx.x; q < p.rows; q += AP_STREAM_THREADS) {
         float a = s_m[0][q], b = s_s[0][q];
         for (int w = 1; w < AP_STREAM_THREADS / 64; w++) ap_lse_join<false>(a, b, s_m[w][q], s_s[w][q], f);
-        p.part[(int64_t)blockIdx.x * p.rows + q] = make_float2(a, b);
+        p.part[(int64_t)blockIdx.x * p.all + q] = make_float2(a, b);
     }
 }
 
@@ -476,19 +478,41 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
         else GX::each(acc, [&](int i, int j, float v) { if (i < queries && j < cols) unsafeAtomicAdd(to + (int64_t)i * p.dim + j, v); });
         return;
     }
+    // The columns are the product's rows: a lane then holds four of them in a row of one document.  They leave through LDS in whole lines, half a tile
+    // of f32 at a time: what 16 lanes hold of 4 documents by themselves are 32 bytes each, and memory writes these no faster than lines.
     uint32_t m, n;
-    ap_g_tile(blockIdx.x - p.runs * mt * nt, (p.count + TM - 1) / TM, nt, nt, &m, &n);
-    const int32_t m0 = m * TM, n0 = n * TN, docs = min(TM, p.count - m0), cols = min(TN, p.dim - n0);
-    GD::product({p.c + (int64_t)m0 * SIZE, p.ldc, docs * SIZE}, {p.x + n0 * SIZE, p.ldx, cols * SIZE}, p.rows, p.parts, p.c_part, p.x_part, lds, acc);
+    ap_g_tile(blockIdx.x - p.runs * mt * nt, (p.count + TN - 1) / TN, (p.dim + TM - 1) / TM, (p.dim + TM - 1) / TM, &n, &m);
+    const int32_t m0 = m * TM, n0 = n * TN, docs = min(TN, p.count - n0), cols = min(TM, p.dim - m0);
+    GD::product({p.x + m0 * SIZE, p.ldx, cols * SIZE}, {p.c + (int64_t)n0 * SIZE, p.ldc, docs * SIZE}, p.rows, p.parts, p.x_part, p.c_part, lds, acc);
     float f1 = p.scale, f2 = *p.most;
     if (PARTS) { f1 = ldexpf(f1, -AP_COEF_UP); f2 = ldexpf(f2, -ap_loss_up(p.amax[1])); }
-    const int64_t at0 = (p.first + m0) * p.ld_out + n0;
-    GD::each(acc, [&](int i, int j, float v) {
-        if (i >= docs || j >= cols) return;
-        v = v * f1 * f2;
-        if (F32) __builtin_nontemporal_store(v, static_cast<float *>(p.grad_docs) + at0 + i * p.ld_out + j);
-        else __builtin_nontemporal_store((__bf16)v, static_cast<__bf16 *>(p.grad_docs) + at0 + i * p.ld_out + j);
-    });
+    constexpr int OUT = F32 ? 4 : 2, LINE = TM * OUT, GROUPS = LINE / 16, HALVES = TN * LINE > GD::LDS_BYTES ? 2 : 1, FH = GD::FB / HALVES, DH = TN / HALVES;
+    char *const to = static_cast<char *>(p.grad_docs) + ((p.first + n0) * p.ld_out + m0) * OUT;
+#pragma unroll
+    for (int h = 0; h < HALVES; h++) {
+        // the documents of this half: blocks h FH .. of every wave, which lie together in LDS
+        const int wave_doc = ap_wave_id() % WN * (DH / WN);
+#pragma unroll
+        for (int b = 0; b < FH; b++)
+#pragma unroll
+            for (int a = 0; a < GD::FA; a++) {
+                const int doc = wave_doc + b * 16 + (threadIdx.x & 15), at = GD::row(a) * OUT, group = (at >> 4) ^ (doc & (GROUPS < 16 ? GROUPS - 1 : 15));
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; r++) v[r] = acc[a][h * FH + b][r] * f1 * f2;
+                if constexpr (F32) *reinterpret_cast<float4 *>(lds + doc * LINE + group * 16) = make_float4(v[0], v[1], v[2], v[3]);
+                else *reinterpret_cast<uint2 *>(lds + doc * LINE + group * 16 + (at & 15)) = make_uint2(ap_bf16_pair(v[0], v[1]), ap_bf16_pair(v[2], v[3]));
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < DH * GROUPS; i += GD::THREADS) {
+            const int at = i / GROUPS, group = i % GROUPS, doc = at / (DH / WN) * (TN / WN) + h * (DH / WN) + at % (DH / WN);
+            if (doc >= docs || group * (16 / OUT) >= cols) continue;
+            typedef uint32_t words __attribute__((ext_vector_type(4)));
+            __builtin_nontemporal_store(*reinterpret_cast<const words *>(lds + at * LINE + (group ^ (at & (GROUPS < 16 ? GROUPS - 1 : 15))) * 16),
+                                        reinterpret_cast<words *>(to + doc * p.ld_out * OUT + group * 16));
+        }
+        __syncthreads();
+    }
 }
 
 // The sums of many runs: 16 threads share an element's.
@@ -706,19 +730,25 @@ static int check_sizes(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
     return AP_OK;
 }
 
-// Up to how many queries one pass over the documents pays.
-static bool loss_few(int64_t rows, int32_t dim, int32_t dtype) { return rows <= 64 && ap_stream_lds(rows, (int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) <= AP_STREAM_LDS; }
-
+// Up to how many queries passes over the documents pay.  A step over 120,011 bf16 rows of 1,024: 371 us by passes and 453 by tiles for 48 queries, 454 and 469
+// for 64; over 30,522 of 768: 101 and 108, 121 and 110.  Over 100,000 f32 rows of 768: 565 and 637 for 64; over 20,000 of 384: 75 and 80 for 48, 90 and 81 for 64.
+#define AP_LOSS_FEW_F32 64
+#define AP_LOSS_FEW_BF16 48
+static int32_t few_group(int64_t row_bytes) { return (int32_t)std::min<int64_t>(64, AP_STREAM_LDS / ((row_bytes + 63) / 64 * 64) / 16 * 16); }   // queries a pass
+static bool loss_few(int64_t rows, int32_t dim, int32_t dtype) {
+    const int64_t most = g_ap_debug.loss_few ? std::min<int64_t>(g_ap_debug.loss_few - 1, 64) : dtype == AP_BF16 ? AP_LOSS_FEW_BF16 : AP_LOSS_FEW_F32;
+    return rows <= most && few_group((int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) > 0;
+}
 // How rows are multiplied: bf16 as they are; f32 as they are by the f32 instruction, or as two f16 parts each.  Parts cost two passes over the documents
-// and two launches more, and save most of a product's time (about 330 against 90 TFLOP/s): they pay from r queries with 8 fs r n dim above
-// 20 us + 2.6 ps n dim on (step of 100 over 2,000 of 128: 31 us in f32, 75 in parts; of 2,048 over 100,000 of 768: 9.9 and 4.1 ms).  The loss and its
-// gradient go by the same rule: a logit that is off is then off in both.
+// and two launches more, and save most of a product's time.  A step over 100,000 rows of 768 takes 838 us in f32 and 829 in parts for 128 queries, 1,441
+// and 949 for 200; over 20,000 of 384, 119 and 130, and 233 and 152; 100 queries over 2,000 of 128, 41 and 75.  The loss and its gradient go by the
+// same rule: a logit that is off is then off in both.
 enum LossForm { LOSS_BF16, LOSS_F32, LOSS_PARTS };
 static LossForm form_of(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
     if (dtype == AP_BF16) return LOSS_BF16;
     const double work = (double)n * dim;
     if (g_ap_debug.loss_form) return g_ap_debug.loss_form == 1 ? LOSS_F32 : LOSS_PARTS;
-    return loss_few(rows, dim, dtype) || 16e-15 * rows * work < 20e-6 + 1.6e-12 * work ? LOSS_F32 : LOSS_PARTS;
+    return loss_few(rows, dim, dtype) || rows <= 128 + 3.75e8 / work ? LOSS_F32 : LOSS_PARTS;
 }
 
 struct LossParts {   // f32 rows as two f16 parts
@@ -766,19 +796,28 @@ static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
     return AP_OK;
 }
 
-template <int DT, bool GRAD> static int launch_few(const ApLoss &p, hipStream_t st) {
-    // the pairs of the waves take the queries' place
-    const size_t lds = (size_t)std::max<int64_t>(ap_stream_lds(p.rows, (int64_t)p.dim * (DT == AP_F32 ? 4 : 2)), div_up(p.rows, 16) * 16 * 8 * (AP_STREAM_THREADS / 64));
-    const int64_t blocks = ap_stream_blocks(p.count);
-    const dim3 grid((unsigned)blocks);
+template <int DT, bool GRAD> static int launch_few(const ApLoss &all, hipStream_t st) {
+    const int64_t row_bytes = (int64_t)all.dim * (DT == AP_F32 ? 4 : 2), blocks = ap_stream_blocks(all.count);
+    const int32_t group = few_group(row_bytes);
+    for (int32_t q0 = 0; q0 < all.rows; q0 += group) {   // as many queries at a time as LDS holds
+        ApLoss p = all;
+        p.all = all.rows;
+        p.rows = std::min(group, all.rows - q0);
+        p.x += q0 * p.ldx;
+        p.labels += q0;
+        if (GRAD) { p.coef += q0; p.lse += q0; p.c += q0 * 4; } else { p.part += q0; p.at_label += q0; }
+        // the pairs of the waves take the queries' place
+        const size_t lds = (size_t)std::max<int64_t>(ap_stream_lds(p.rows, row_bytes), div_up(p.rows, 16) * 16 * 8 * (AP_STREAM_THREADS / 64));
+        const dim3 grid((unsigned)blocks);
 #define AP_FEW(N)                                                                                                                       \
     case N:                                                                                                                             \
         if (lds > 60 * 1024) AP_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_loss_few<DT, N, GRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
-        hipLaunchKernelGGL((k_loss_few<DT, N, GRAD>), grid, dim3(AP_STREAM_THREADS), lds, st, p);                                             \
+        hipLaunchKernelGGL((k_loss_few<DT, N, GRAD>), grid, dim3(AP_STREAM_THREADS), lds, st, p);                                       \
         break
-    switch ((p.rows + 15) / 16) { AP_FEW(1); AP_FEW(2); AP_FEW(3); AP_FEW(4); }
+        switch ((p.rows + 15) / 16) { AP_FEW(1); AP_FEW(2); AP_FEW(3); AP_FEW(4); }
 #undef AP_FEW
-    AP_CHECK_HIP(hipGetLastError());
+        AP_CHECK_HIP(hipGetLastError());
+    }
     return AP_OK;
 }
 
@@ -849,9 +888,10 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
 
 
 // In how many runs of its documents the queries' gradient is made, so that its workgroups (`tiles` a run, taken first) and the `more` of the documents'
-// gradient, `k` long, end together on 256 compute units.  A workgroup costs its length and about 512 for its start and end.
-static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k, int64_t parts, int64_t *cost_of = nullptr) {
-    const int64_t cus = 256, over = 512;
+// gradient, `k` long, end together on 256 compute units (two small tiles each).  A workgroup costs its length and some more for its start and end: about 512
+// for tiles of 256, 256 for smaller ones, and 48 of the longer f32 steps.
+static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k, int64_t parts, int tile, LossForm form, int64_t *cost_of = nullptr) {
+    const int64_t cus = tile == 256 ? 256 : 512, over = form == LOSS_F32 ? 48 : tile == 256 ? 512 : 256;
     int32_t best = 1;
     int64_t least = INT64_MAX;
     for (int32_t s = 1; s <= 32 && (s == 1 || piece / s >= 256); s++) {
@@ -884,7 +924,7 @@ struct GradPlan {
         const int64_t tc = pick_tile(p, r, form), t = pick_tile(p, dim, form), more = div_up(p, t) * div_up(dim, t);
         double cost = (double)(div_up(div_up(p, tc) * div_up(r, tc), 256) * (dim * parts + 512)) * tc * tc / 65536;
         int64_t least = div_up(more, 256) * (r * parts + 512);
-        if (want_x) pick_runs(div_up(r, t) * div_up(dim, t), p, more, r, parts, &least);
+        if (want_x) pick_runs(div_up(r, t) * div_up(dim, t), p, more, r, parts, (int)t, form, &least);
         return cost + (double)least * t * t / 65536 + 2 * 2048;   // two launches
     }
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype, bool want_x) {
@@ -911,7 +951,9 @@ struct GradPlan {
         else if (piece < n) {   // several pieces: the length of which all of them take the least time
             double least = 1e30;
             int64_t best = piece;
+            const int tile_of_all = pick_tile(piece, dim, form);   // the largest tiles take a length of which they fill the compute units
             for (int64_t p = piece; p >= piece / 2 && p >= 256; p -= up_to(piece / 32, 256)) {
+                if (pick_tile(p, dim, form) != tile_of_all) break;
                 const double t = (double)(n / p) * piece_cost(p, r, dim, parts, want_x, form) + (n % p ? piece_cost(up_to(n % p, 256), r, dim, parts, want_x, form) : 0);
                 if (t < least) { least = t; best = p; }
             }
@@ -926,7 +968,7 @@ struct GradPlan {
         tile = pick_tile(piece, dim, form);
         if (tile > 128 && r <= 128) tile = 128;
         if (tile > 64 && r <= 64) tile = 64;
-        runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts);
+        runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts, tile, form);
         run_docs = (int32_t)up_to(div_up(piece, runs), 64);
         runs = (int32_t)div_up(piece, run_docs);
         most = ws.take<float>(1);
