@@ -19,7 +19,6 @@
 
 #define AP_LOG2E 1.44269504088896340736f
 #define AP_LOG2E_LO 1.92596299112661746887e-8f   // log2(e) - AP_LOG2E
-#define AP_LN2 0.69314718055994530942f
 #define AP_COEF_UP 14                            // f16 coefficients are stored times 2^14: they are at most 1
 
 // ------------------------------------------------------------------ f32 rows as two f16 parts
@@ -129,6 +128,8 @@ struct ApFactor {
         if (amax) { a = ldexpf(a, -ap_loss_up(amax[0])); b = ldexpf(b, -ap_loss_up(amax[1])); }
     }
     template <bool PARTS> __device__ __forceinline__ float of(float v) const { return PARTS ? v * a * b : v * a; }
+    template <bool PARTS> __device__ __forceinline__ float less(float v, float of_it) const { return fmaf(PARTS ? v * b : v, a, -of_it); }   // b is a power of two: one rounding, of the difference
+    __device__ __forceinline__ double exact(float v) const { return (double)v * a * b; }
 };
 
 __device__ __forceinline__ uint32_t ap_bf16_pair(float a, float b) {
@@ -144,11 +145,11 @@ template <bool PARTS> __device__ __forceinline__ void ap_lse_join(float &m, floa
     m = t;
 }
 
-// A coefficient out of a logit times log2(e), for a query of weight g (0: none).
+// A coefficient out of a product, for a query of weight g (0: none).
 struct ApCoef {
     float g, lse2, lse2_lo;
     __device__ __forceinline__ ApCoef(float g_, float lse) : g(g_), lse2(lse * AP_LOG2E) { lse2_lo = fmaf(lse, AP_LOG2E, -lse2) + lse * AP_LOG2E_LO; }
-    __device__ __forceinline__ float exp_of(float v) const { return __builtin_amdgcn_exp2f((v - lse2) - lse2_lo); }
+    template <bool PARTS> __device__ __forceinline__ float exp_of(float v, const ApFactor &f) const { return __builtin_amdgcn_exp2f(f.less<PARTS>(v, lse2) - lse2_lo); }
     __device__ __forceinline__ float times(float e) const { return g != 0.f ? e * g : 0.f; }   // e: the exponential, less 1 at the label
 };
 // Four coefficients as 16-bit numbers (f16: times 2^AP_COEF_UP); what they are off by stays in v.
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
 #pragma unroll
             for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) acc[a][b][r] = coef.exp_of(f.of<PARTS>(acc[a][b][r]));
+                for (int r = 0; r < 4; r++) acc[a][b][r] = coef.template exp_of<PARTS>(acc[a][b][r], f);
             if (local >= 0 && local < TM / WM && !(local & 12)) {
 #pragma unroll
                 for (int a = 0; a < G::FA; a++)
@@ -310,10 +311,10 @@ __global__ __launch_bounds__(1024) void k_loss_join(const float2 *__restrict__ p
         }
     }
     if ((int)threadIdx.x < 1 << qb && q < rows) {
-        const float sum = log2f(s);
-        lse[q] = (f.of<true>(m) + sum) * AP_LN2;
+        const double sum = (double)log2f(s), ln2 = 0.693147180559945309417;
+        lse[q] = (float)((f.exact(m) + sum) * ln2);   // one rounding: what lse is off by, every coefficient of the query is off by
         const int32_t label = labels[q];
-        loss[q] = label >= 0 && label < n ? (f.of<true>(m - at_label[q]) + sum) * AP_LN2 : 0.f;
+        loss[q] = label >= 0 && label < n ? (float)((f.exact(m - at_label[q]) + sum) * ln2) : 0.f;
     }
 }
 
@@ -358,7 +359,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
                 float v[4];
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const float e = co.exp_of(f.of<false>(acc[g][r])) - (label[g] == p.first + d + r ? 1.f : 0.f);
+                    const float e = co.exp_of<false>(acc[g][r], f) - (label[g] == p.first + d + r ? 1.f : 0.f);
                     v[r] = d + r < p.count ? co.times(e) : 0.f;
                 }
                 const int all = (p.all + 15) / 16 * 16;
