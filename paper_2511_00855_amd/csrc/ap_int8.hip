@@ -87,8 +87,16 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) 
         if (lane == 0) s_scale[q] = s;
     }
     __syncthreads();
+    struct Four { float v[4]; };
     ap_stream<ApStreamI8, NQ>(p.q, p.ldq, p.n, p.pad, lds, (int64_t)blockIdx.x * (AP_STREAM_THREADS / 64) + wave, (int64_t)gridDim.x * (AP_STREAM_THREADS / 64),
-                              [&](int64_t first, const ap_g_i32x4 (&acc)[NQ]) {
+                              [&](int64_t first) {
+                                  const int64_t d = first + (lane >> 4) * 4;
+                                  Four s;
+#pragma unroll
+                                  for (int r = 0; r < 4; r++) s.v[r] = p.q_scale[d + r < p.n ? d + r : p.n - 1];
+                                  return s;
+                              },
+                              [&](int64_t first, const ap_g_i32x4 (&acc)[NQ], const Four &s) {
                                   const int64_t d = first + (lane >> 4) * 4;
 #pragma unroll
                                   for (int g = 0; g < NQ; g++) {
@@ -96,7 +104,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) 
                                       if (q >= p.rows) continue;
 #pragma unroll
                                       for (int r = 0; r < 4; r++)
-                                          if (d + r < p.n) p.out[q * p.ld_out + d + r] = (float)acc[g][r] * s_scale[q] * p.q_scale[d + r];
+                                          if (d + r < p.n) p.out[q * p.ld_out + d + r] = (float)acc[g][r] * s_scale[q] * s.v[r];
                                   }
                               });
 }

@@ -148,9 +148,13 @@ template <bool PARTS> __device__ __forceinline__ void ap_lse_join(float &m, floa
 // A coefficient out of a product, for a query of weight g (0: none).
 struct ApCoef {
     float g, lse2, lse2_lo;
-    __device__ __forceinline__ ApCoef(float g_, float lse) : g(g_), lse2(lse * AP_LOG2E) { lse2_lo = fmaf(lse, AP_LOG2E, -lse2) + lse * AP_LOG2E_LO; }
-    template <bool PARTS> __device__ __forceinline__ float exp_of(float v, const ApFactor &f) const { return __builtin_amdgcn_exp2f(f.less<PARTS>(v, lse2) - lse2_lo); }
-    __device__ __forceinline__ float times(float e) const { return g != 0.f ? e * g : 0.f; }   // e: the exponential, less 1 at the label
+    // a query of weight 0 may have an lse that is no number; its products are 0
+    __device__ __forceinline__ ApCoef(float g_, float lse) : g(g_), lse2(g_ != 0.f ? lse * AP_LOG2E : 0.f) { lse2_lo = g_ != 0.f ? fmaf(lse, AP_LOG2E, -lse2) + lse * AP_LOG2E_LO : 0.f; }
+    // EXACT: with the last bits of lse, which a coefficient in bf16 does not show
+    template <bool PARTS, bool EXACT> __device__ __forceinline__ float exp_of(float v, const ApFactor &f) const {
+        return __builtin_amdgcn_exp2f(EXACT ? f.less<PARTS>(v, lse2) - lse2_lo : f.less<PARTS>(v, lse2));
+    }
+    __device__ __forceinline__ float times(float e) const { return e * g; }   // e: the exponential, less 1 at the label
 };
 // Four coefficients as 16-bit numbers (f16: times 2^AP_COEF_UP); what they are off by stays in v.
 template <bool F16> __device__ __forceinline__ uint2 ap_coef_part(float (&v)[4]) {
@@ -226,7 +230,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
 #pragma unroll
             for (int a = 0; a < G::FA; a++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) acc[a][b][r] = coef.template exp_of<PARTS>(acc[a][b][r], f);
+                for (int r = 0; r < 4; r++) acc[a][b][r] = coef.template exp_of<PARTS, std::is_same<OP, ApBf16Op>::value == false>(acc[a][b][r], f);
             if (local >= 0 && local < TM / WM && !(local & 12)) {
 #pragma unroll
                 for (int a = 0; a < G::FA; a++)
@@ -350,7 +354,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
             coef[g] = q < p.rows ? p.coef[q] : 0.f;
             lse[g] = q < p.rows ? p.lse[q] : 0.f;
         }
-        ap_stream<OP, NQ>(p.docs + p.first * p.ldd, p.ldd, p.count, bytes, lds, wave0, waves, [&](int64_t first, const ap_s_f32x4 (&acc)[NQ]) {
+        ap_stream<OP, NQ>(p.docs + p.first * p.ldd, p.ldd, p.count, bytes, lds, wave0, waves, [](int64_t) { return 0; }, [&](int64_t first, const ap_s_f32x4 (&acc)[NQ], int) {
             const int64_t d = first + (lane >> 4) * 4;
 #pragma unroll
             for (int g = 0; g < NQ; g++) {
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
                 float v[4];
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const float e = co.exp_of<false>(acc[g][r], f) - (label[g] == p.first + d + r ? 1.f : 0.f);
+                    const float e = co.template exp_of<false, true>(acc[g][r], f) - (label[g] == p.first + d + r ? 1.f : 0.f);
                     v[r] = d + r < p.count ? co.times(e) : 0.f;
                 }
                 const int all = (p.all + 15) / 16 * 16;
@@ -370,8 +374,8 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
         });
         return;
     }
-    ap_stream<OP, NQ>(p.docs, p.ldd, p.count, bytes, lds, wave0, waves,
-                      [&](int64_t first, const ap_s_f32x4 (&acc)[NQ]) {
+    ap_stream<OP, NQ>(p.docs, p.ldd, p.count, bytes, lds, wave0, waves, [](int64_t) { return 0; },
+                      [&](int64_t first, const ap_s_f32x4 (&acc)[NQ], int) {
                           const int64_t d = first + (lane >> 4) * 4;
 #pragma unroll
                           for (int g = 0; g < NQ; g++) {
@@ -995,16 +999,18 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, ApLossGrad g, int64_t n, 
     for (int64_t d0 = 0; d0 < n; d0 += plan.piece) {
         p.first = g.first = d0;
         p.count = g.count = (int32_t)std::min(plan.piece, n - d0);
-        AP_TRY((launch_tiles<OP, PARTS, true>(p, plan.tile_c, st)));
-        const int64_t nt = div_up(g.dim, plan.tile);
+        // a short last piece may take smaller tiles
+        AP_TRY((launch_tiles<OP, PARTS, true>(p, std::min(plan.tile_c, pick_tile(p.count, p.rows, plan.form)), st)));
+        const int tile = std::min(plan.tile, pick_tile(g.count, g.dim, plan.form));
+        const int64_t nt = div_up(g.dim, tile);
         g.run_docs = plan.run_docs;
         g.start = d0 == 0;
         // a short last piece leaves the runs past its end alone
         g.runs = (uint32_t)(!g.gx ? 0 : g.start ? plan.runs : div_up(g.count, plan.run_docs));
-        const dim3 grid((unsigned)(g.runs * div_up(g.rows, plan.tile) * nt + (g.grad_docs ? div_up(g.count, plan.tile) * nt : 0)));
-        if (plan.tile == 256) {
+        const dim3 grid((unsigned)(g.runs * div_up(g.rows, tile) * nt + (g.grad_docs ? div_up(g.count, tile) * nt : 0)));
+        if (tile == 256) {
             if constexpr (OP::BYTES == 2) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
-        } else if (plan.tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        } else if (tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         else hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         AP_CHECK_HIP(hipGetLastError());
     }
@@ -1067,7 +1073,7 @@ extern "C" int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, co
     g.c = plan.c; g.most = plan.most; g.grad_docs = grad_docs; g.ld_out = dim; g.gx = plan.gx; g.dim = dim;
     if (plan.few) {
         ApLoss q = p;
-        q.docs = static_cast<const char *>(docs); q.x = static_cast<const char *>(x); q.ldd = ldd * size; q.ldx = ldx * size; q.dim = dim;
+        q.docs = static_cast<const char *>(docs); q.x = plan.x; q.ldd = ldd * size; q.ldx = dim * size; q.dim = dim;
         const ApLossFew f{q.docs, plan.x, q.ldd, dim * size, reinterpret_cast<const float *>(plan.c), 0, 0, (int32_t)rows, dim, scale, plan.most, grad_docs, plan.gx, 0, 0};
         AP_TRY((dtype == AP_BF16 ? few_pieces<AP_BF16>(plan, q, f, n, st) : few_pieces<AP_F32>(plan, q, f, n, st)));
         const int64_t total = rows * dim / 4;

@@ -49,14 +49,15 @@ static inline int64_t ap_stream_lds(int64_t rows, int64_t row_bytes) { return (r
 // Where byte `at` of query q lies in LDS, of `nq` groups of 16 queries.
 __device__ __forceinline__ int ap_stream_place(int q, int at, int nq) { return (((at >> 6) * nq + (q >> 4)) * 64 + ((at >> 4) & 3) * 16 + (q & 15)) * 16 + (at & 15); }
 
-// Calls done(first row, acc) for every 16 rows that this wave takes; acc[g][r]: row first + 4 (lane / 16) + r, query 16 g + lane % 16.
-// Rows past the last are the last row again.
-template <class OP, int NQ, class F>
-__device__ __forceinline__ void ap_stream(const char *rows, int64_t ld, int64_t n, int32_t row_bytes, const char *lds, int64_t wave, int64_t waves, F done) {
+// Calls done(first row, acc, with) for every 16 rows that this wave takes; acc[g][r]: row first + 4 (lane / 16) + r, query 16 g + lane % 16.
+// Rows past the last are the last row again.  `with` is what before(first row) has read ahead for them.
+template <class OP, int NQ, class B, class F>
+__device__ __forceinline__ void ap_stream(const char *rows, int64_t ld, int64_t n, int32_t row_bytes, const char *lds, int64_t wave, int64_t waves, B before, F done) {
     const int lane = threadIdx.x & 63, part = (lane >> 4) * 16, steps = (row_bytes + 63) / 64;
     for (int64_t first = wave * 16; first < n; first += waves * 16) {
         const int64_t row = first + (lane & 15);
         const char *p = rows + (row < n ? row : n - 1) * ld;
+        const auto with = before(first);
         typename OP::Acc sums[NQ][OP::SUMS];
 #pragma unroll
         for (int g = 0; g < NQ; g++)
@@ -83,7 +84,7 @@ __device__ __forceinline__ void ap_stream(const char *rows, int64_t ld, int64_t 
         typename OP::Acc acc[NQ];
 #pragma unroll
         for (int g = 0; g < NQ; g++) acc[g] = OP::sum(sums[g]);
-        done(first, acc);
+        done(first, acc, with);
     }
 }
 #endif
