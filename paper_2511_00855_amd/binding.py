@@ -8,6 +8,7 @@ There is no fallback: if the library is missing or a call fails, this raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -111,6 +112,7 @@ def calibration_copy(dst: torch.Tensor, src: torch.Tensor):
 def debug_set(name: str, value: int):
     """A debug setting of the library (see ap_debug_set); 0 restores the library's own choice."""
     _check(lib().ap_debug_set(name.encode(), C.c_int64(int(value))), "ap_debug_set")
+    _bytes_of.cache_clear()
 
 
 DEBUG_NAMES = ("seed_sample_cols", "seed_buffer_cap", "seed_tau_ulps", "max_launch_threads", "search_workspace_bytes",
@@ -547,6 +549,14 @@ def _vec(t: torch.Tensor, dtype, count: int, device, what: str):
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=256)
+def _bytes_of(fn: str, args) -> int:
+    """What ap_<fn>_bytes(*args) says: the same for the same sizes, until a debug setting changes."""
+    need = C.c_size_t()
+    _check(getattr(lib(), fn + "_bytes")(*args, C.byref(need)), fn + "_bytes")
+    return need.value
+
+
 def _call(fn: str, device, *args, bytes_args=None):
     """Calls ap_<fn> on the device's current stream, with the workspace that ap_<fn>_bytes(*bytes_args) asks for."""
     if torch.cuda.current_device() != device.index:
@@ -554,10 +564,9 @@ def _call(fn: str, device, *args, bytes_args=None):
             return _call(fn, device, *args, bytes_args=bytes_args)
     L = lib()
     if bytes_args is not None:
-        need = C.c_size_t()
-        _check(getattr(L, fn + "_bytes")(*bytes_args, C.byref(need)), fn + "_bytes")
-        ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None   # held until the call has been made
-        args += (None if ws is None else ws.data_ptr(), need.value)
+        need = _bytes_of(fn, bytes_args)
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None   # held until the call has been made
+        args += (None if ws is None else ws.data_ptr(), need)
     _check(getattr(L, fn)(*args, torch._C._cuda_getCurrentRawStream(device.index)), fn)
 
 

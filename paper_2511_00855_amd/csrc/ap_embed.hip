@@ -259,19 +259,21 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
     if (group < groups) put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), group * N, sum);
 }
 
-// Stable radix sort of the entries by token: 2,048 entries a block, up to 9 bits a pass.  What names no row of the table sorts last.
-#define AP_SORT_ITEMS 2048
+// Stable radix sort of the entries by token, up to 9 bits a pass.  What names no row of the table sorts last.  A block takes `items` entries: 512, which
+// are two rounds of its waves, up to 2^18 entries (160,000: a scatter 20 us with 79 blocks of 2,048), 2,048 of more, where the counts of
+// the blocks would cost more than their rounds.
+#define AP_SORT_ITEMS(n) ((n) > (1 << 18) ? 2048 : 512)
 #define AP_SORT_BINS 512
 __device__ __forceinline__ uint32_t sort_key(const int32_t *tokens, int64_t vocab, int64_t i) { const int32_t t = tokens[i]; return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab; }
 
 // keys: NULL in the first pass, which takes the tokens
-__global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ tokens, int64_t vocab, const uint32_t *__restrict__ keys, int64_t n, int shift, int bits, uint32_t *__restrict__ hist,
-                                                    int64_t blocks) {
+__global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ tokens, int64_t vocab, const uint32_t *__restrict__ keys, int64_t n, int items, int shift, int bits,
+                                                    uint32_t *__restrict__ hist, int64_t blocks) {
     __shared__ uint32_t s_cnt[AP_SORT_BINS];
     for (int b = threadIdx.x; b < 1 << bits; b += 256) s_cnt[b] = 0;
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * AP_SORT_ITEMS;
-    for (int i = threadIdx.x; i < AP_SORT_ITEMS && i0 + i < n; i += 256) {
+    const int64_t i0 = (int64_t)blockIdx.x * items;
+    for (int i = threadIdx.x; i < items && i0 + i < n; i += 256) {
         const uint32_t k = keys ? keys[i0 + i] : sort_key(tokens, vocab, i0 + i);
         atomicAdd(&s_cnt[(k >> shift) & ((1 << bits) - 1)], 1u);
     }
@@ -307,7 +309,7 @@ static int list_rows(const ApEmbed &p, int32_t *row, hipStream_t st) {
     return AP_OK;
 }
 // The last pass also brings along what the sums need of an entry: its row (-1: none) and its weight.
-__global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t *__restrict__ keys, const int32_t *__restrict__ entries, int shift, int bits, const uint32_t *__restrict__ hist,
+__global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t *__restrict__ keys, const int32_t *__restrict__ entries, int items, int shift, int bits, const uint32_t *__restrict__ hist,
                                                       int64_t blocks, const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys_out, int32_t *__restrict__ entries_out, int last,
                                                       const int32_t *__restrict__ row_in, int32_t *__restrict__ row_out, float *__restrict__ w_out) {
     __shared__ uint32_t s_at[4][AP_SORT_BINS], s_first[AP_SORT_BINS], s_wave[4];
@@ -325,8 +327,8 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t 
         s_first[b + 1] = sum - y;
     }
     __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * AP_SORT_ITEMS + wave * (AP_SORT_ITEMS / 4);   // a wave's entries lie together
-    for (int i = lane; i < AP_SORT_ITEMS / 4; i += 64)
+    const int64_t i0 = (int64_t)blockIdx.x * items + wave * (items / 4);   // a wave's entries lie together
+    for (int i = lane; i < items / 4; i += 64)
         if (i0 + i < p.n) atomicAdd(&s_at[wave][((keys ? keys[i0 + i] : sort_key(p.tokens, p.vocab, i0 + i)) >> shift) & mask], 1u);
     __syncthreads();
     for (uint32_t b = threadIdx.x; b <= mask; b += 256) {
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t 
         for (int w = 0; w < 4; w++) { const uint32_t c = s_at[w][b]; s_at[w][b] = at; at += c; }
     }
     __syncthreads();
-    for (int i = 0; i < AP_SORT_ITEMS / 4; i += 64) {
+    for (int i = 0; i < items / 4; i += 64) {
         if (i0 + i >= p.n) break;
         const bool is = i0 + i + lane < p.n;
         const uint32_t k = !is ? 0 : keys ? keys[i0 + i + lane] : sort_key(p.tokens, p.vocab, i0 + i + lane), d = (k >> shift) & mask;
@@ -604,7 +606,7 @@ struct GradWs {
         while ((1ll << all) <= vocab) all++;   // keys 0 .. vocab
         passes = (int32_t)div_up(all, 9);
         bits = (int32_t)div_up(all, passes);
-        blocks = div_up(n, AP_SORT_ITEMS);
+        blocks = div_up(n, AP_SORT_ITEMS(n));
         run = 64;   // as long as they fill the compute units: every run leaves two rows of sums behind
         while (run < 256 && n / run > AP_RUNS) run *= 2;
         runs = div_up(n, run);
@@ -637,6 +639,7 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     GradWs ws;
     const size_t need = embed_few(lists->n) ? 0 : ws.lay(static_cast<char *>(workspace), lists->n, vocab, dim);
     AP_REQUIRE(bytes >= need && (workspace || need == 0), "workspace of %zu bytes, %zu are needed", bytes, need);
+    AP_REQUIRE(((uintptr_t)workspace & 255) == 0, "workspace must be 256-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(stream);
     ApEmbed p = args_of(grad_out, ld, dtype, vocab, dim, lists, scale, grad_table);
     const int64_t words = vocab * dim / (table_dtype == AP_BF16 ? 8 : 4);
@@ -654,12 +657,14 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
         return AP_OK;
     }
     if (lists->indptr) AP_TRY(list_rows(p, ws.rows_in, st));
+    const int items = AP_SORT_ITEMS(lists->n);
     for (int i = 0; i < ws.passes; i++) {
         const uint32_t *keys = i ? ws.keys[(i - 1) & 1] : nullptr;
         const int32_t *entries = i ? ws.entries[(i - 1) & 1] : nullptr;
-        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, keys, lists->n, i * ws.bits, ws.bits, ws.hist, ws.blocks);
+        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, keys, lists->n, items, i * ws.bits, ws.bits, ws.hist,
+                           ws.blocks);
         hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)div_up(1 << ws.bits, 4)), dim3(256), 0, st, ws.hist, ws.blocks, 1 << ws.bits, ws.totals);
-        hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, keys, entries, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.totals, ws.keys[i & 1],
+        hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, keys, entries, items, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.totals, ws.keys[i & 1],
                            ws.entries[i & 1], i + 1 == ws.passes, lists->indptr ? ws.rows_in : nullptr, ws.rows, ws.w);
         AP_CHECK_HIP(hipGetLastError());
     }
@@ -705,6 +710,7 @@ extern "C" int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t 
     weights_layout(lists->n, dim, dtype, grad_dtype, &slabs, &part_bytes, &row_bytes);
     const size_t need = part_bytes + row_bytes;
     AP_REQUIRE(bytes >= need && (workspace || need == 0), "workspace of %zu bytes, %zu are needed", bytes, need);
+    AP_REQUIRE(((uintptr_t)workspace & 255) == 0, "workspace must be 256-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (lists->rows == 0) return ap_fill_u32(grad_weights, (size_t)lists->n, 0, st);
     const ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, nullptr);

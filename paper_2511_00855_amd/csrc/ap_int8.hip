@@ -251,6 +251,7 @@ extern "C" int ap_scores_int8(const void *x, int64_t ldx, const float *x_scale, 
     size_t need;
     AP_TRY(ap_scores_int8_bytes(rows, dim, x_dtype, &need));
     AP_REQUIRE(bytes >= need && (workspace || need == 0), "workspace of %zu bytes, %zu are needed", bytes, need);
+    AP_REQUIRE(((uintptr_t)workspace & 255) == 0, "workspace must be 256-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(stream);
     ApScores8 p{static_cast<const char *>(x), ldx * size_of(x_dtype), x_scale, reinterpret_cast<const char *>(q), ldq, q_scale, (int32_t)rows, (int32_t)n, dim, pad, out, ld_out, 8};
     if (scores8_few(rows, pad)) return x_dtype == AP_I8 ? few<AP_I8>(p, st) : x_dtype == AP_BF16 ? few<AP_BF16>(p, st) : few<AP_F32>(p, st);

@@ -866,6 +866,7 @@ extern "C" int ap_softmax_loss(const void *x, int64_t ldx, int64_t rows, const v
     LossPlan plan;
     const size_t need = plan.lay(static_cast<char *>(workspace), rows, n, dim, dtype);
     AP_REQUIRE(workspace && bytes >= need, "workspace of %zu bytes, %zu are needed", bytes, need);
+    AP_REQUIRE(((uintptr_t)workspace & 255) == 0, "workspace must be 256-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(stream);
     ApLoss p{};
     p.count = (int32_t)n; p.rows = (int32_t)rows; p.scale = scale; p.labels = labels; p.part = plan.part; p.at_label = plan.at_label;
@@ -1052,6 +1053,7 @@ extern "C" int ap_softmax_loss_grad(const void *x, int64_t ldx, int64_t rows, co
     GradPlan plan;
     const size_t need = plan.lay(static_cast<char *>(workspace), rows, n, dim, dtype, grad_x != nullptr);
     AP_REQUIRE(workspace && bytes >= need, "workspace of %zu bytes, %zu are needed", bytes, need);
+    AP_REQUIRE(((uintptr_t)workspace & 255) == 0, "workspace must be 256-byte aligned");
     const bool parts = plan.form == LOSS_PARTS;
     const int64_t size = dtype == AP_BF16 ? 2 : 4;
     const int32_t groups = (int32_t)(dim * size / 16);

@@ -103,6 +103,51 @@ def test_pieces_of_the_documents(debug_knobs, dtype, rows, n, dim):
         assert all(torch.equal(a, b) for a, b in zip(whole[:2], got[:2]))
 
 
+@pytest.mark.parametrize("form", [1, 2])
+@pytest.mark.parametrize("few", [0, 1])
+@pytest.mark.parametrize("rows,n,dim", [(20, 300, 68), (64, 515, 260), (150, 700, 100), (1, 64, 8192)])
+def test_forms_of_f32_products(debug_knobs, form, few, rows, n, dim):
+    """The f32 instruction and the two f16 parts, tiles and passes over the documents, whatever the sizes would choose."""
+    debug_knobs("loss_form", form)
+    debug_knobs("loss_few", few)
+    rng = np.random.default_rng(n)
+    x, docs, labels = make(rng, rows, n, dim, F32)
+    check(x, docs, labels, 6.0, torch.full((rows,), 1.0 / rows, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_queries_by_the_ten_thousand(dtype):
+    """More queries than every workgroup looks through for the largest weight."""
+    rng = np.random.default_rng(8)
+    x, docs, labels = make(rng, 17_000, 90, 24, dtype)
+    labels[5], labels[16_999] = -1, 90
+    check(x, docs, labels, 5.0, torch.from_numpy(rng.uniform(-1.0, 1.0, 17_000).astype(np.float32)).to(DEV))
+
+
+@pytest.mark.parametrize("rows", [3, 130])
+def test_documents_past_32_bits(rows):
+    """Documents of more than 2^32 bytes: labels among the last are found, and the gradient reaches them."""
+    n, dim = 2_100_003, 1024
+    docs = torch.zeros((n, dim), dtype=BF16, device=DEV)
+    g = torch.Generator(DEV).manual_seed(1)
+    docs[-300:] = (torch.randn((300, dim), generator=g, device=DEV) * dim ** -0.5).to(BF16)
+    x = (docs[-rows:].float() * 0.5).to(BF16)
+    labels = torch.arange(n - rows, n, dtype=torch.int32, device=DEV)
+    loss, lse = B.softmax_loss(x, docs, labels, scale=20.0)
+    gx, gd = B.softmax_loss_grad(x, docs, labels, lse, torch.ones(rows, device=DEV), scale=20.0)
+    logits = 20.0 * (x.double() @ docs[-300:].double().T)
+    want = torch.logsumexp(torch.cat([logits, torch.full((rows, 1), float(np.log(n - 300)), device=DEV, dtype=torch.float64)], 1), 1)
+    own = logits[torch.arange(rows), 300 - rows + torch.arange(rows)]
+    assert (lse.double() - want).abs().max() < 2e-5 and (loss.double() - (want - own)).abs().max() < 2e-5   # 2^-19 (1 + |lse|), twice the logits' sums
+    c = torch.exp(logits - want[:, None])
+    c[torch.arange(rows), 300 - rows + torch.arange(rows)] -= 1.0
+    size = 20.0 * (c.abs() @ docs[-300:].double().abs())
+    assert ((gx.double() - 20.0 * (c @ docs[-300:].double())).abs() <= 2.0 ** -7 * size).all()
+    wd = 20.0 * (c.T @ x.double())
+    assert ((gd[-300:].double() - wd).abs() <= 2.0 ** -7 * 20.0 * (c.T.abs() @ x.double().abs())).all()
+    assert torch.isfinite(gd[:1000]).all() and (gd[:1000].double() - 20.0 * (torch.exp(-want) @ x.double())).abs().max() <= 2.0 ** -7 * 20.0 * float((torch.exp(-want) @ x.double().abs()).max())
+
+
 @pytest.mark.parametrize("want", [(True, False), (False, True)])
 @pytest.mark.parametrize("dtype,rows", [(BF16, 200), (F32, 9)])
 def test_one_gradient_alone(dtype, rows, want):
