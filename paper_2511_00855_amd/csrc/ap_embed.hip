@@ -175,14 +175,17 @@ __device__ __forceinline__ int64_t row_of(const int64_t *indptr, int64_t rows, i
 }
 
 #define AP_EMBED_FEW 4096   // entries that find their equals by reading the list
-// Few entries, one launch.  The first `owners` workgroups: a wave takes an entry and 1 KB of its columns; if no earlier entry names the same token it
-// adds up all that do, in order.  The others write zeros where no token points; which rows those are they see from a bitmap of the tokens (of
-// `bits` rows; 0: somebody else has written the zeros).
+// Few entries, one launch.  The first `owners` workgroups: one takes an entry and four slabs of 256 bytes, a wave each.  If no earlier entry names the
+// same token, it lists those that do, in order, with their rows and weights, and adds them up, 16 lanes every fourth of them.  (A frequent token has
+// a tenth of all entries: rows asked for as they are found, 64 entries at a time, took 60 us of 3,000.)  The other workgroups write
+// zeros where no token points; which rows those are they see from a bitmap of the tokens (of `bits` rows; 0: somebody else has written the
+// zeros).
 template <int GT, int OT>
 __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owners, int32_t bits) {
     constexpr int N = ApRow16<GT>::N;
     extern __shared__ int32_t s_few[];
-    const int lane = threadIdx.x & 63;
+    __shared__ int32_t s_count[4];
+    const int lane = threadIdx.x & 63, wave = ap_wave_id();
     if ((int32_t)blockIdx.x >= owners) {
         uint32_t *map = reinterpret_cast<uint32_t *>(s_few);
         for (int i = threadIdx.x; i < (bits + 31) / 32; i += 256) map[i] = 0;
@@ -204,59 +207,64 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
         }
         return;
     }
-    // the tokens and, of each, its list: looked up when a token has been found would be a chain of reads for every 64 entries
-    int32_t *s_row = s_few + p.n;
-    for (int i = threadIdx.x; i < p.n; i += 256) { s_few[i] = p.tokens[i]; s_row[i] = p.indptr ? -1 : i; }
-    __syncthreads();
-    if (p.indptr)
-        for (int64_t r = threadIdx.x >> 4; r < p.rows; r += 16) {
-            if (!ap_row_ok(p.indptr, r, p.n)) continue;
-            const int end = (int)p.indptr[r + 1];
-            for (int e = (int)p.indptr[r] + (threadIdx.x & 15); e < end; e += 16) s_row[e] = (int32_t)r;
-        }
-    __syncthreads();
-    const int groups = p.dim / N, slabs = (groups + 63) / 64;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int e0 = (int)(unit / slabs);
-    if (e0 >= p.n) return;
-    const int32_t t = s_few[e0];
+    const int quads = (p.dim / N + 63) / 64, n = (int)p.n;   // of slabs
+    const int e0 = blockIdx.x / quads;
+    const int32_t t = p.tokens[e0];
     if (t < 0 || t >= p.vocab) return;
     bool earlier = false;
-    for (int e = lane; e < e0; e += 64) earlier |= s_few[e] == t;
-    if (__any(earlier)) return;
-    const int group = (int)(unit % slabs) * 64 + lane;
+    for (int e = threadIdx.x; e < e0; e += 256) earlier |= p.tokens[e] == t;
+    if (__syncthreads_or(earlier)) return;
+    // the list: each wave a run of the entries, its places behind the earlier waves'
+    int32_t *s_row = s_few;
+    float *s_w = reinterpret_cast<float *>(s_few + n);
+    const int each = ((n - e0 + 3) / 4 + 63) / 64 * 64, b = e0 + wave * each, end = min(n, b + each);
+    int count = 0;
+    for (int e = b; e < end; e += 64) count += __popcll(__ballot(e + lane < end && p.tokens[e + lane] == t));
+    if (lane == 0) s_count[wave] = count;
+    __syncthreads();
+    int at = 0, all = 0;
+    for (int w = 0; w < 4; w++) { if (w < wave) at += s_count[w]; all += s_count[w]; }
+    for (int e = b; e < end; e += 64) {
+        const bool same = e + lane < end && p.tokens[e + lane] == t;
+        const uint64_t m = __ballot(same);
+        if (same) {
+            const int k = at + __popcll(m & ((1ull << lane) - 1)), row = (int)row_of(p.indptr, p.rows, e + lane);
+            s_row[k] = row;
+            s_w[k] = row >= 0 ? p.scale * (p.weights ? p.weights[e + lane] : 1.f) : 0.f;
+        }
+        at += __popcll(m);
+    }
+    __syncthreads();
+    const int32_t col = ((blockIdx.x % quads * 4 + wave) * 16 + (lane & 15)) * N;
+    const bool mine = col < p.dim;
+    const char *from = p.table + (mine ? col : 0) * (16 / N);
     float sum[N];
 #pragma unroll
-    for (int i = 0; i < N; i++) sum[i] = 0.f;
-    for (int e = e0; e < p.n; e += 64) {
-        const bool same = e + lane < p.n && s_few[e + lane] == t;
-        if (!__any(same)) continue;
-        int64_t row = -1;
-        float w = 0.f;
-        if (same) { row = s_row[e + lane]; w = p.scale * (p.weights ? p.weights[e + lane] : 1.f); }
-        for (uint64_t m = __ballot(row >= 0); m;) {   // eight rows on their way at a time: a frequent token has many
-            uint4 v[8];
-            float wk[8];
+    for (int j = 0; j < N; j++) sum[j] = 0.f;
+    for (int k0 = lane >> 4; k0 < all; k0 += 32) {
+        uint4 v[8];
+        float w[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                v[i] = make_uint4(0, 0, 0, 0);
-                wk[i] = 0.f;
-                if (!m) continue;
-                const int k = __ffsll((unsigned long long)m) - 1;
-                m &= m - 1;
-                wk[i] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k));
-                if (group < groups) v[i] = *reinterpret_cast<const uint4 *>(p.table + (int64_t)__builtin_amdgcn_readlane((int32_t)row, k) * p.ld + group * 16);
-            }
+        for (int i = 0; i < 8; i++) {
+            const int k = k0 + i * 4, row = k < all ? s_row[k] : -1;
+            w[i] = row >= 0 ? s_w[k] : 0.f;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (row >= 0) v[i] = *reinterpret_cast<const uint4 *>(from + row * p.ld);
+        }
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                float x[N];
-                ApRow16<GT>::get(v[i], x);
+        for (int i = 0; i < 8; i++) {
+            float x[N];
+            ApRow16<GT>::get(v[i], x);
 #pragma unroll
-                for (int j = 0; j < N; j++) sum[j] = fmaf(wk[i], x[j], sum[j]);
-            }
+            for (int j = 0; j < N; j++) sum[j] = fmaf(w[i], x[j], sum[j]);
         }
     }
-    if (group < groups) put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), group * N, sum);
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+        sum[j] += __shfl_xor(sum[j], 16, 64);
+        sum[j] += __shfl_xor(sum[j], 32, 64);
+    }
+    if (mine && lane < 16) put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), col, sum);
 }
 
 // Stable radix sort of the entries by token, up to 9 bits a pass.  What names no row of the table sorts last.  A block takes `items` entries: 512, which
@@ -648,7 +656,7 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     AP_CHECK_HIP(hipGetLastError());
     if (!any) return AP_OK;
     if (few) {
-        const int32_t owners = (int32_t)div_up(lists->n * div_up(dim / (dtype == AP_BF16 ? 8 : 4), 64), 4), bits = one ? (int32_t)vocab : 0;
+        const int32_t owners = (int32_t)(lists->n * div_up(dim / (dtype == AP_BF16 ? 8 : 4), 64)), bits = one ? (int32_t)vocab : 0;
         const size_t lds = std::max<size_t>((size_t)lists->n * 8, (size_t)(bits + 31) / 32 * 4);
         const dim3 grid((unsigned)(owners + (one ? std::min<int64_t>(div_up(words, 1024), 1024) : 0)));
 #define AP_FEW(A, B) hipLaunchKernelGGL((k_embed_grad_few<A, B>), grid, dim3(256), lds, st, p, owners, bits)
