@@ -735,13 +735,14 @@ static int check_sizes(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
     return AP_OK;
 }
 
-// Up to how many queries passes over the documents pay.  A step over 120,011 bf16 rows of 1,024: 371 us by passes and 453 by tiles for 48 queries, 454 and 469
-// for 64; over 30,522 of 768: 101 and 108, 121 and 110.  Over 100,000 f32 rows of 768: 565 and 637 for 64; over 20,000 of 384: 75 and 80 for 48, 90 and 81 for 64.
-#define AP_LOSS_FEW_F32 64
-#define AP_LOSS_FEW_BF16 48
+// Up to how many queries passes over the documents pay.  bf16, the loss of 64: 51 us by passes and 57 by tiles over 120,011 rows of 1,024, 136 and 207 over
+// 500,000 of 768; a step: 32 queries over 120,011 of 1,024, 259 and 421, 40 queries 364 and 296, and over 30,522 of 768, 82 and 98, 98 and 87.  f32: a step of
+// 64 over 100,000 rows of 768 566 and 629; over 20,000 of 384, 74 and 78 for 48, 91 and 80 for 64.  f32 takes the same way for the loss and its gradient (form_of).
+#define AP_LOSS_FEW 64
+#define AP_LOSS_FEW_GRAD_BF16 32
 static int32_t few_group(int64_t row_bytes) { return (int32_t)std::min<int64_t>(64, AP_STREAM_LDS / ((row_bytes + 63) / 64 * 64) / 16 * 16); }   // queries a pass
-static bool loss_few(int64_t rows, int32_t dim, int32_t dtype) {
-    const int64_t most = g_ap_debug.loss_few ? std::min<int64_t>(g_ap_debug.loss_few - 1, 64) : dtype == AP_BF16 ? AP_LOSS_FEW_BF16 : AP_LOSS_FEW_F32;
+static bool loss_few(int64_t rows, int32_t dim, int32_t dtype, bool grad) {
+    const int64_t most = g_ap_debug.loss_few ? std::min<int64_t>(g_ap_debug.loss_few - 1, 64) : dtype == AP_BF16 && grad ? AP_LOSS_FEW_GRAD_BF16 : AP_LOSS_FEW;
     return rows <= most && few_group((int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) > 0;
 }
 // How rows are multiplied: bf16 as they are; f32 as they are by the f32 instruction, or as two f16 parts each.  Parts cost two passes over the documents
@@ -753,7 +754,7 @@ static LossForm form_of(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
     if (dtype == AP_BF16) return LOSS_BF16;
     const double work = (double)n * dim;
     if (g_ap_debug.loss_form) return g_ap_debug.loss_form == 1 ? LOSS_F32 : LOSS_PARTS;
-    return loss_few(rows, dim, dtype) || rows <= 128 + 3.75e8 / work ? LOSS_F32 : LOSS_PARTS;
+    return loss_few(rows, dim, dtype, false) || rows <= 128 + 3.75e8 / work ? LOSS_F32 : LOSS_PARTS;
 }
 
 struct LossParts {   // f32 rows as two f16 parts
@@ -837,7 +838,7 @@ struct LossPlan {
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
         LossWs ws{base};
         form = form_of(rows, n, dim, dtype);
-        few = loss_few(rows, dim, dtype) && form != LOSS_PARTS;
+        few = loss_few(rows, dim, dtype, false) && form != LOSS_PARTS;
         tile = pick_tile(n, rows, form);
         pairs = few ? ap_stream_blocks(n) : div_up(n, tile);
         part = ws.take<float2>(pairs * rows);
@@ -938,7 +939,7 @@ struct GradPlan {
         const int64_t r = std::max<int64_t>(rows, 1);
         form = form_of(r, n, dim, dtype);
         const int64_t parts = form == LOSS_PARTS ? 3 : 1, size = form == LOSS_F32 ? 4 : 2;
-        few = loss_few(r, dim, dtype) && form != LOSS_PARTS;
+        few = loss_few(r, dim, dtype, true) && form != LOSS_PARTS;
         if (few) {   // workgroups of a whole number of 16 documents, as many as there are compute units
             const int64_t r16 = up_to(r, 16);
             piece = std::min<int64_t>(AP_LOSS_PIECE_BYTES / (r16 * 4) / 256 * 256, up_to(n, 16));
@@ -973,7 +974,7 @@ struct GradPlan {
         tile_c = pick_tile(piece, r, form);
         tile = pick_tile(piece, dim, form);
         if (tile > 128 && r <= 128) tile = 128;
-        if (tile > 64 && r <= 64) tile = 64;
+        if (tile > 64 && r <= 64 && form == LOSS_F32) tile = 64;   // 64 queries over 100,000 f32 rows of 768: 629 us, 741 with 128; 64 over 120,011 bf16 rows of 1,024: 465, 325 with 128
         runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts, tile, form);
         run_docs = (int32_t)up_to(div_up(piece, runs), 64);
         runs = (int32_t)div_up(piece, run_docs);
