@@ -166,6 +166,20 @@ __global__ __launch_bounds__(256) void k_embed_zero(uint4 *__restrict__ p, int64
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = make_uint4(0, 0, 0, 0);
 }
 
+// Zeros to the rows that no entry names: 16 lanes a row.
+__global__ __launch_bounds__(256) void k_embed_zero_unnamed(char *__restrict__ out, int64_t row_bytes, int64_t vocab, const uint8_t *__restrict__ named) {
+    const int64_t groups = (int64_t)gridDim.x * 16;
+    for (int64_t r = blockIdx.x * (int64_t)16 + (threadIdx.x >> 4); r < vocab; r += groups * 4) {
+        bool is[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) is[k] = r + k * groups < vocab && !named[r + k * groups];
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            if (is[k])
+                for (int64_t c = (threadIdx.x & 15) * 16; c < row_bytes; c += 256) *reinterpret_cast<uint4 *>(out + (r + k * groups) * row_bytes + c) = make_uint4(0, 0, 0, 0);
+    }
+}
+
 // The list that entry e lies in, -1 for none.
 __device__ __forceinline__ int64_t row_of(const int64_t *indptr, int64_t rows, int64_t e) {
     if (!indptr) return e;
@@ -270,20 +284,29 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
 // Stable radix sort of the entries by token, up to 9 bits a pass.  What names no row of the table sorts last.  A block takes `items` entries: 512, which
 // are two rounds of its waves, up to 2^18 entries (160,000: a scatter 20 us with 79 blocks of 2,048), 2,048 of more, where the counts of
 // the blocks would cost more than their rounds.
-#define AP_SORT_ITEMS(n) ((n) > (1 << 18) ? 2048 : 512)
+#define AP_SORT_SOME 512
+#define AP_SORT_MANY 2048
+#define AP_SORT_ITEMS(n) ((n) > (1 << 18) ? AP_SORT_MANY : AP_SORT_SOME)
 #define AP_SORT_BINS 512
 __device__ __forceinline__ uint32_t sort_key(const int32_t *tokens, int64_t vocab, int64_t i) { const int32_t t = tokens[i]; return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab; }
 
-// keys: NULL in the first pass, which takes the tokens
-__global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ tokens, int64_t vocab, const uint32_t *__restrict__ keys, int64_t n, int items, int shift, int bits,
+// pairs: NULL in the first pass, which takes the tokens
+__global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ tokens, int64_t vocab, const uint2 *__restrict__ pairs, int64_t n, int items, int shift, int bits,
                                                     uint32_t *__restrict__ hist, int64_t blocks) {
     __shared__ uint32_t s_cnt[AP_SORT_BINS];
     for (int b = threadIdx.x; b < 1 << bits; b += 256) s_cnt[b] = 0;
     __syncthreads();
     const int64_t i0 = (int64_t)blockIdx.x * items;
-    for (int i = threadIdx.x; i < items && i0 + i < n; i += 256) {
-        const uint32_t k = keys ? keys[i0 + i] : sort_key(tokens, vocab, i0 + i);
-        atomicAdd(&s_cnt[(k >> shift) & ((1 << bits) - 1)], 1u);
+    for (int i = threadIdx.x; i < items; i += 1024) {
+        uint32_t k[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int64_t e = i0 + i + j * 256;
+            k[j] = i + j * 256 < items && e < n ? pairs ? pairs[e].x : sort_key(tokens, vocab, e) : 0xffffffffu;   // no key has these bits
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            if (k[j] != 0xffffffffu) atomicAdd(&s_cnt[(k[j] >> shift) & ((1 << bits) - 1)], 1u);
     }
     __syncthreads();
     for (int b = threadIdx.x; b < 1 << bits; b += 256) hist[b * blocks + blockIdx.x] = s_cnt[b];
@@ -293,12 +316,17 @@ __global__ __launch_bounds__(256) void k_sort_scan(uint32_t *__restrict__ hist, 
     const int lane = threadIdx.x & 63, bin = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (bin >= bins) return;
     uint32_t *h = hist + bin * blocks, before = 0;
-    for (int64_t i = 0; i < blocks; i += 64) {
-        const uint32_t own = i + lane < blocks ? h[i + lane] : 0;
-        uint32_t sum = own;
-        for (int o = 1; o < 64; o <<= 1) { const uint32_t t = __shfl_up(sum, o, 64); if (lane >= o) sum += t; }
-        if (i + lane < blocks) h[i + lane] = before + sum - own;
-        before += __shfl(sum, 63, 64);
+    for (int64_t i = 0; i < blocks; i += 256) {
+        uint32_t own[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) own[k] = i + k * 64 + lane < blocks ? h[i + k * 64 + lane] : 0;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            uint32_t sum = own[k];
+            for (int o = 1; o < 64; o <<= 1) { const uint32_t t = __shfl_up(sum, o, 64); if (lane >= o) sum += t; }
+            if (i + k * 64 + lane < blocks) h[i + k * 64 + lane] = before + sum - own[k];
+            before += __shfl(sum, 63, 64);
+        }
     }
     if (lane == 0) totals[bin] = before;
 }
@@ -316,58 +344,109 @@ static int list_rows(const ApEmbed &p, int32_t *row, hipStream_t st) {
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }
-// The last pass also brings along what the sums need of an entry: its row (-1: none) and its weight.
-__global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, const uint32_t *__restrict__ keys, const int32_t *__restrict__ entries, int items, int shift, int bits, const uint32_t *__restrict__ hist,
-                                                      int64_t blocks, const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys_out, int32_t *__restrict__ entries_out, int last,
-                                                      const int32_t *__restrict__ row_in, int32_t *__restrict__ row_out, float *__restrict__ w_out) {
-    __shared__ uint32_t s_at[4][AP_SORT_BINS], s_first[AP_SORT_BINS], s_wave[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// An entry goes along as its key, its row (-1: none) and, if there are any, its weight.  A block's entries are put in order in LDS and leave by it: a wave
+// writes a bin's entries together and not 64 places.  1.2M entries of 250,002 tokens: both passes 77 us unordered and with rows and weights looked up by the last,
+// 42 us so.
+struct ApSorted { uint2 *of; float *w; };   // of: key and row, after the last pass row and weight
+template <int ITEMS>
+__global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, int shift, int bits, const uint32_t *__restrict__ hist, int64_t blocks, const uint32_t *__restrict__ totals, int last,
+                                                      const int32_t *__restrict__ rows, uint32_t *__restrict__ keys_out, ApSorted out, uint8_t *__restrict__ named /* or NULL */) {
+    __shared__ uint32_t s_at[4][AP_SORT_BINS], s_base[AP_SORT_BINS], s_wave[2][4];
+    __shared__ uint2 s_of[ITEMS];
+    __shared__ float s_w[ITEMS];
+    constexpr int EACH = ITEMS / 256;
+    const int64_t b0 = (int64_t)blockIdx.x * ITEMS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, count = (int)min((int64_t)ITEMS, p.n - b0);
     const uint32_t mask = (1u << bits) - 1;
-    for (int b = threadIdx.x; b < 4 * AP_SORT_BINS; b += 256) (&s_at[0][0])[b] = 0;
-    {   // where the bins begin: two of them a thread
-        const uint32_t b = threadIdx.x * 2, x = b <= mask ? totals[b] : 0, y = b + 1 <= mask ? totals[b + 1] : 0;
-        uint32_t sum = x + y;
-        for (int o = 1; o < 64; o <<= 1) { const uint32_t v = __shfl_up(sum, o, 64); if (lane >= o) sum += v; }
-        if (lane == 63) s_wave[wave] = sum;
-        __syncthreads();
-        for (int w = 0; w < wave; w++) sum += s_wave[w];
-        s_first[b] = sum - x - y;
-        s_first[b + 1] = sum - y;
-    }
-    __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * items + wave * (items / 4);   // a wave's entries lie together
-    for (int i = lane; i < items / 4; i += 64)
-        if (i0 + i < p.n) atomicAdd(&s_at[wave][((keys ? keys[i0 + i] : sort_key(p.tokens, p.vocab, i0 + i)) >> shift) & mask], 1u);
-    __syncthreads();
-    for (uint32_t b = threadIdx.x; b <= mask; b += 256) {
-        uint32_t at = s_first[b] + hist[b * blocks + blockIdx.x];
+    const int i0 = wave * (ITEMS / 4) + lane;   // a wave's entries lie together
+    const bool weighted = p.weights != nullptr;
+    uint2 own[EACH];                            // all asked for at once
+    float w[EACH];
 #pragma unroll
-        for (int w = 0; w < 4; w++) { const uint32_t c = s_at[w][b]; s_at[w][b] = at; at += c; }
+    for (int k = 0; k < EACH; k++) {
+        const int64_t e = b0 + i0 + k * 64;
+        own[k] = make_uint2(0, 0);
+        w[k] = 1.f;
+        if (i0 + k * 64 >= count) continue;
+        if (in.of) {
+            own[k] = in.of[e];
+            if (weighted) w[k] = in.w[e];
+        } else {
+            own[k] = make_uint2(sort_key(p.tokens, p.vocab, e), rows ? (uint32_t)rows[e] : (uint32_t)e);
+            if (weighted) w[k] = p.weights[e];
+        }
+    }
+    for (int b = threadIdx.x; b < 4 * AP_SORT_BINS; b += 256) (&s_at[0][0])[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < EACH; k++)
+        if (i0 + k * 64 < count) atomicAdd(&s_at[wave][(own[k].x >> shift) & mask], 1u);
+    __syncthreads();
+    {   // where the bins begin, here and among all: two of them a thread
+        const uint32_t b = threadIdx.x * 2;
+        uint32_t here_of[2] = {0, 0}, all[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            if (b + k <= mask) all[k] = totals[b + k];
+#pragma unroll
+            for (int w = 0; w < 4; w++) here_of[k] += s_at[w][b + k];
+        }
+        uint32_t here = here_of[0] + here_of[1], sum = all[0] + all[1];
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t v = __shfl_up(here, o, 64), u = __shfl_up(sum, o, 64);
+            if (lane >= o) { here += v; sum += u; }
+        }
+        if (lane == 63) { s_wave[0][wave] = here; s_wave[1][wave] = sum; }
+        __syncthreads();
+        for (int w = 0; w < wave; w++) { here += s_wave[0][w]; sum += s_wave[1][w]; }
+        here -= here_of[0] + here_of[1];
+        sum -= all[0] + all[1];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            if (b + k <= mask) s_base[b + k] = sum + hist[(b + k) * blocks + blockIdx.x] - here;   // modulo 2^32
+            uint32_t at = here;
+#pragma unroll
+            for (int w = 0; w < 4; w++) { const uint32_t c = s_at[w][b + k]; s_at[w][b + k] = at; at += c; }
+            here += here_of[k];
+            sum += all[k];
+        }
     }
     __syncthreads();
-    for (int i = 0; i < items / 4; i += 64) {
-        if (i0 + i >= p.n) break;
-        const bool is = i0 + i + lane < p.n;
-        const uint32_t k = !is ? 0 : keys ? keys[i0 + i + lane] : sort_key(p.tokens, p.vocab, i0 + i + lane), d = (k >> shift) & mask;
+#pragma unroll
+    for (int k = 0; k < EACH; k++) {
+        const bool is = i0 + k * 64 < count;
+        const uint32_t d = (own[k].x >> shift) & mask;
         uint64_t same = __ballot(is);
         for (int b = 0; b < bits; b++) { const uint64_t m = __ballot((d >> b) & 1); same &= (d >> b) & 1 ? m : ~m; }
         uint32_t at = 0;
-        if (is) at = s_at[wave][d] + __popcll(same & ((1ull << lane) - 1));
+        if (is) { at = s_at[wave][d] + __popcll(same & ((1ull << lane) - 1)); s_of[at] = own[k]; s_w[at] = w[k]; }
         ap_wave_sync();
         if (is && (same >> lane) == 1) s_at[wave][d] = at + 1;   // the last lane of its digit
         ap_wave_sync();
-        if (is) {
-            const int64_t e = entries ? entries[i0 + i + lane] : i0 + i + lane;
-            keys_out[at] = k;
-            if (!last) entries_out[at] = (int32_t)e;
-            else { row_out[at] = row_in ? row_in[e] : (int32_t)e; w_out[at] = p.scale * (p.weights ? p.weights[e] : 1.f); }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < EACH; k++) {
+        const int i = threadIdx.x + k * 256;
+        if (i >= count) break;
+        const uint2 v = s_of[i];
+        const uint32_t at = s_base[(v.x >> shift) & mask] + i;
+        if (last) {
+            keys_out[at] = v.x;
+            out.of[at] = make_uint2(v.y, __float_as_uint(p.scale * s_w[i]));
+            if (named && v.x < p.vocab && (i == 0 || s_of[i - 1].x != v.x)) named[v.x] = 1;   // equal tokens lie together
+        } else {
+            out.of[at] = v;
+            if (weighted) out.w[at] = s_w[i];
         }
     }
 }
 
 // 16 lanes take a run of `run` sorted entries and a slab.  Tokens whose entries all lie in the run are written; the sum of a token that began
 // in an earlier run goes to carry[run][0], that of one that goes on in the next to carry[run][1].
-struct ApRuns { const uint32_t *keys; const int32_t *rows; const float *w; float *carry; int32_t run; };
+struct ApRuns { const uint32_t *keys; const uint2 *of; float *carry; int32_t run; int64_t runs; };   // of: an entry's row and weight
+// carry[column / 64][which][run][column % 64]: what the joining reads of a token's runs lies together
+__device__ __forceinline__ float *carry_at(const ApRuns &s, int64_t run, int which, int32_t col) { return s.carry + ((col / 64 * 2 + which) * s.runs + run) * 64 + col % 64; }
 template <int GT, int OT>
 __global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, ApSlabs sl) {
     constexpr int N = ApRow16<GT>::N;
@@ -389,8 +468,9 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, Ap
         const bool is = e + l16 < end;
         const uint32_t key = is ? s.keys[e + l16] : 0xffffffffu;
         const uint32_t next = e + l16 + 1 < p.n ? s.keys[e + l16 + 1] : 0xffffffffu;
-        const int32_t row = is && key < p.vocab ? s.rows[e + l16] : -1;   // -1 also for an entry of no list
-        const float w = row >= 0 ? s.w[e + l16] : 0.f;
+        const uint2 of = is && key < p.vocab ? s.of[e + l16] : make_uint2(0xffffffffu, 0u);
+        const int32_t row = (int32_t)of.x;   // -1 also for an entry of no list
+        const float w = row >= 0 ? __uint_as_float(of.y) : 0.f;
         // 1: the token's sum ends here, 2: it goes on in the next run
         const int32_t what = is && key < p.vocab ? (next != key ? 1 : e + l16 + 1 == end ? 2 : 0) : 0;
         for_each_const<2>([&](auto half) {
@@ -411,8 +491,8 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, Ap
                 if (!end_k) return;
                 const int32_t t = row_bcast<K0 + k>((int32_t)key);
                 if (mine) {
-                    if (begun) put_row<AP_F32, N>(s.carry + run * 2 * p.dim, col, sum);
-                    else if (end_k == 2) put_row<AP_F32, N>(s.carry + (run * 2 + 1) * p.dim, col, sum);
+                    if (begun) put_row<AP_F32, N>(carry_at(s, run, 0, col), 0, sum);
+                    else if (end_k == 2) put_row<AP_F32, N>(carry_at(s, run, 1, col), 0, sum);
                     else put_row<OT, N>(p.out + (int64_t)t * p.dim * (OT == AP_F32 ? 4 : 2), col, sum);
                 }
 #pragma unroll
@@ -422,54 +502,70 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, Ap
         });
     }
 }
-// A wave for each run whose last token goes on adds up the sums of the runs that it lies in; the four waves of a workgroup share the runs of a
-// token that lies in many.
-#define AP_JOIN_ALONE 32
+// 16 lanes take a run whose last token goes on and add up the sums of the runs that the token lies in: if these are 16 at most, in the first `wide`
+// workgroups of 16 runs, 256 columns at a time; the others in workgroups of their own for 64 columns, whose 16 groups share them.  Everything
+// here waits for memory: keys and probes are asked for together.  (A tenth of 1.2M entries are 940 runs of 128: a wave a run, 256 columns and a
+// search by halves took 56 us, 28 us so.)
 template <int OT>
-__global__ __launch_bounds__(256) void k_embed_grad_join(ApEmbed p, ApRuns s, int64_t runs) {
-    __shared__ float4 s_sum[4][64];
-    __shared__ int64_t s_lo[4];
-    const int lane = threadIdx.x & 63, wave = ap_wave_id();
-    const int64_t first = (int64_t)blockIdx.x * 4, run = first + wave, last = run * s.run + s.run - 1;   // the run's last entry
+__global__ __launch_bounds__(256) void k_embed_grad_join(ApEmbed p, ApRuns s, int32_t wide) {
+    __shared__ float4 s_sum[16][16];
+    __shared__ int64_t s_lo[16];
+    const int l16 = threadIdx.x & 15, sub = threadIdx.x >> 4;
+    const bool many = (int32_t)blockIdx.y >= wide;
+    const int64_t first = (int64_t)blockIdx.x * 16, run = first + sub, last = run * s.run + s.run - 1;   // the run's last entry
     int64_t lo = 0;   // the runs that begin with its token: run + 1 .. lo - 1; 0: nothing to do
     if (last + 1 < p.n) {
-        const uint32_t t = s.keys[last];
-        if (t < p.vocab && s.keys[last + 1] == t && !(run > 0 && s.keys[run * s.run] == t && s.keys[run * s.run - 1] == t)) {   // goes on, and began here
-            lo = run + 1;
-            for (int64_t hi = runs; lo < hi;) { const int64_t m = (lo + hi) / 2; if (s.keys[m * s.run] == t) lo = m + 1; else hi = m; }
-        }
+        const int64_t near = run + 1 + l16;
+        const uint32_t t = s.keys[last], here = s.keys[run * s.run], before = run > 0 ? s.keys[run * s.run - 1] : 0xffffffffu, probe = near < s.runs ? s.keys[near * s.run] : 0xffffffffu;
+        const int same = __popc((uint32_t)(__ballot(probe == t) >> (threadIdx.x & 48)) & 0xffffu);
+        // goes on, and began here
+        if (t < p.vocab && same > 0 && !(here == t && before == t) && many == (same == 16)) lo = run + 1 + same;
     }
-    if (lane == 0) s_lo[wave] = lo;
-    __syncthreads();
-    for (int c0 = blockIdx.y * 64; c0 * 4 < p.dim; c0 += gridDim.y * 64) {
-        const int c = (c0 + lane) * 4;
-        auto add = [&](int64_t b, int64_t end, float4 sum) {
-#pragma unroll 8
-            for (int64_t r = b; r < end; r++) {
-                const float4 v = *reinterpret_cast<const float4 *>(s.carry + r * 2 * p.dim + c);
-                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-            }
-            return sum;
-        };
-        auto put = [&](int64_t of, const float4 &sum) {
-            const float v[4] = {sum.x, sum.y, sum.z, sum.w};
-            put_row<OT, 4>(p.out + (int64_t)s.keys[of * s.run + s.run - 1] * p.dim * (OT == AP_F32 ? 4 : 2), c, v);
-        };
-        for (int w = 0; w < 4; w++) {
-            const int64_t of = first + w, to = s_lo[w], count = to - of - 1;
-            if (to == 0 || (count <= AP_JOIN_ALONE && w != wave)) continue;
-            if (count <= AP_JOIN_ALONE) {
-                if (c < p.dim) put(of, add(of + 1, to, *reinterpret_cast<const float4 *>(s.carry + (of * 2 + 1) * p.dim + c)));
-                continue;
-            }
-            const int64_t each = (count + 3) / 4, b = of + 1 + wave * each;
+    if (many) {
+        if (!__syncthreads_or(lo != 0)) return;
+        // the first run that begins with another token: 16 probes at a time
+        for (int64_t hi = lo ? s.runs : 0; lo < hi;) {
+            const int64_t step = (hi - lo + 15) / 16, m = lo + l16 * step;
+            const int k = __popc((uint32_t)(__ballot(m < hi && s.keys[m * s.run] == s.keys[last]) >> (threadIdx.x & 48)) & 0xffffu);   // the first k lie in the token
+            if (k < 16) hi = min(hi, lo + k * step);
+            if (k > 0) lo += (k - 1) * step + 1;
+        }
+        if (l16 == 0) s_lo[sub] = lo;
+        __syncthreads();
+    }
+    auto add = [&](int64_t b, int64_t end, int32_t c, float4 sum) {
+        for (; b < end; b += 8) {
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[k] = b + k < end ? *reinterpret_cast<const float4 *>(carry_at(s, b + k, 0, c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; k++) { sum.x += v[k].x; sum.y += v[k].y; sum.z += v[k].z; sum.w += v[k].w; }
+        }
+        return sum;
+    };
+    auto put = [&](int64_t of, int32_t c, const float4 &sum) {
+        const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+        put_row<OT, 4>(p.out + (int64_t)s.keys[of * s.run + s.run - 1] * p.dim * (OT == AP_F32 ? 4 : 2), c, v);
+    };
+    if (!many) {
+        if (lo != 0)
+            for (int32_t c0 = blockIdx.y * 256; c0 < p.dim; c0 += wide * 256)
+                for (int32_t c = c0 + l16 * 4; c < min(c0 + 256, p.dim); c += 64) put(run, c, add(run + 1, lo, c, *reinterpret_cast<const float4 *>(carry_at(s, run, 1, c))));
+        return;
+    }
+    for (int32_t c0 = (blockIdx.y - wide) * 64; c0 < p.dim; c0 += (gridDim.y - wide) * 64) {
+        const int32_t c = c0 + l16 * 4;
+        for (int w = 0; w < 16; w++) {
+            const int64_t of = first + w, to = s_lo[w];
+            if (to == 0) continue;
+            const int64_t each = (to - of - 1 + 15) / 16, b = of + 1 + sub * each;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (c < p.dim) sum = add(b, min(to, b + each), wave ? sum : *reinterpret_cast<const float4 *>(s.carry + (of * 2 + 1) * p.dim + c));
-            s_sum[wave][lane] = sum;
+            if (c < p.dim) sum = add(b, min(to, b + each), c, sub ? sum : *reinterpret_cast<const float4 *>(carry_at(s, of, 1, c)));
+            s_sum[sub][l16] = sum;
             __syncthreads();
-            if (wave == 0 && c < p.dim) {
-                for (int k = 1; k < 4; k++) { const float4 v = s_sum[k][lane]; sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; }
-                put(of, sum);
+            if (sub == 0 && c < p.dim) {
+                for (int k = 1; k < 16; k++) { const float4 v = s_sum[k][l16]; sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w; }
+                put(of, c, sum);
             }
             __syncthreads();
         }
@@ -598,15 +694,18 @@ extern "C" int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vo
     return AP_OK;
 }
 
-#ifndef AP_RUNS
-#define AP_RUNS 16384
-#endif
+#define AP_RUNS 8192   // 1.2M entries x 1,024: runs of 64, 128 and 256 with their joining take 220, 229 and 228 us
+// Whether the rows that entries name are marked, so that zeros go to the others only: not where three quarters are others anyhow.  1.2M entries over 250,002 rows of
+// 2 KB: 39 us of zeros and 4 before the marks instead of 67; 250,000 entries over 100,000: 25 instead of 29.
+#define AP_EMBED_NAMED(n, vocab) ((vocab) <= 4 * (n))
 struct GradWs {
     int64_t blocks, runs;
     int32_t run, passes, bits;
-    uint32_t *keys[2], *hist, *totals;
-    int32_t *entries[2], *rows, *rows_in;
-    float *w, *carry;
+    uint32_t *keys, *hist, *totals;
+    ApSorted sorted[2];
+    int32_t *rows;
+    uint8_t *named;
+    float *carry;
     size_t lay(char *base, int64_t n, int64_t vocab, int32_t dim) {
         size_t at = 0;
         auto take = [&](int64_t count) { char *p = base ? base + at : nullptr; at += (size_t)div_up(count * 4, 256) * 256; return p; };
@@ -618,13 +717,13 @@ struct GradWs {
         run = 64;   // as long as they fill the compute units: every run leaves two rows of sums behind
         while (run < 256 && n / run > AP_RUNS) run *= 2;
         runs = div_up(n, run);
-        for (int i = 0; i < 2; i++) { keys[i] = (uint32_t *)take(n); entries[i] = (int32_t *)take(n); }
+        for (int i = 0; i < 2; i++) { sorted[i].of = (uint2 *)take(2 * n); sorted[i].w = (float *)take(n); }
+        keys = (uint32_t *)take(n);
         hist = (uint32_t *)take(blocks << bits);
         totals = (uint32_t *)take(1ll << bits);
         rows = (int32_t *)take(n);
-        rows_in = (int32_t *)take(n);
-        w = (float *)take(n);
-        carry = (float *)take(runs * 2 * dim);
+        named = AP_EMBED_NAMED(n, vocab) ? (uint8_t *)take(div_up(vocab, 4)) : nullptr;
+        carry = (float *)take(runs * 2 * div_up(dim, 64) * 64);
         return at;
     }
 };
@@ -652,7 +751,8 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
     ApEmbed p = args_of(grad_out, ld, dtype, vocab, dim, lists, scale, grad_table);
     const int64_t words = vocab * dim / (table_dtype == AP_BF16 ? 8 : 4);
     const bool any = lists->n > 0 && lists->rows > 0, few = embed_few(lists->n), one = any && few && vocab <= (1 << 18);   // bits of a bitmap in LDS
-    if (!one) hipLaunchKernelGGL(k_embed_zero, dim3((unsigned)std::min<int64_t>(div_up(words, 256), 8192)), dim3(256), 0, st, static_cast<uint4 *>(grad_table), words);
+    const bool marked = any && !few && AP_EMBED_NAMED(lists->n, vocab);
+    if (!one && !marked) hipLaunchKernelGGL(k_embed_zero, dim3((unsigned)std::min<int64_t>(div_up(words, 256), 8192)), dim3(256), 0, st, static_cast<uint4 *>(grad_table), words);
     AP_CHECK_HIP(hipGetLastError());
     if (!any) return AP_OK;
     if (few) {
@@ -664,27 +764,37 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
 #undef AP_FEW
         return AP_OK;
     }
-    if (lists->indptr) AP_TRY(list_rows(p, ws.rows_in, st));
+    if (marked) AP_TRY(ap_fill_u32(ws.named, (size_t)div_up(vocab, 4), 0, st));
+    if (lists->indptr) AP_TRY(list_rows(p, ws.rows, st));
     const int items = AP_SORT_ITEMS(lists->n);
     for (int i = 0; i < ws.passes; i++) {
-        const uint32_t *keys = i ? ws.keys[(i - 1) & 1] : nullptr;
-        const int32_t *entries = i ? ws.entries[(i - 1) & 1] : nullptr;
-        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, keys, lists->n, items, i * ws.bits, ws.bits, ws.hist,
-                           ws.blocks);
+        const ApSorted in = i ? ws.sorted[(i - 1) & 1] : ApSorted{nullptr, nullptr};
+        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, in.of, lists->n, items, i * ws.bits, ws.bits, ws.hist, ws.blocks);
         hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)div_up(1 << ws.bits, 4)), dim3(256), 0, st, ws.hist, ws.blocks, 1 << ws.bits, ws.totals);
-        hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, keys, entries, items, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.totals, ws.keys[i & 1],
-                           ws.entries[i & 1], i + 1 == ws.passes, lists->indptr ? ws.rows_in : nullptr, ws.rows, ws.w);
+#define AP_SCATTER(ITEMS)                                                                                                                                                    \
+    hipLaunchKernelGGL(k_sort_scatter<ITEMS>, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, in, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.totals, i + 1 == ws.passes, \
+                       lists->indptr ? ws.rows : nullptr, ws.keys, ws.sorted[i & 1], marked ? ws.named : nullptr)
+        if (items == AP_SORT_MANY) AP_SCATTER(AP_SORT_MANY); else AP_SCATTER(AP_SORT_SOME);
+#undef AP_SCATTER
         AP_CHECK_HIP(hipGetLastError());
     }
-    const ApRuns s{ws.keys[(ws.passes - 1) & 1], ws.rows, ws.w, ws.carry, ws.run};
+    if (marked) {
+        const int64_t row_bytes = (int64_t)dim * (table_dtype == AP_BF16 ? 2 : 4);
+        hipLaunchKernelGGL(k_embed_zero_unnamed, dim3((unsigned)std::min<int64_t>(div_up(vocab, 64), 4096)), dim3(256), 0, st, static_cast<char *>(grad_table), row_bytes, vocab, ws.named);
+        AP_CHECK_HIP(hipGetLastError());
+    }
+    const ApRuns s{ws.keys, ws.sorted[(ws.passes - 1) & 1].of, ws.carry, ws.run, ws.runs};
     const ApSlabs sl = slabs_of((int64_t)dim * (dtype == AP_BF16 ? 2 : 4), div_up(ws.runs, 16));
     AP_REQUIRE(slab_blocks(sl) < (1ll << 23), "too many entries");
-    const dim3 grid((unsigned)slab_blocks(sl)), joins((unsigned)div_up(ws.runs, 4), (unsigned)std::max<int64_t>(1, std::min<int64_t>(div_up(dim, 256), (1ll << 25) / ws.runs)));   // below 2^31 threads
+    const dim3 grid((unsigned)slab_blocks(sl));
+    const int64_t heads = div_up(ws.runs, 16), most = (1ll << 22) / heads;   // below 2^31 threads
+    const int32_t wide = (int32_t)std::max<int64_t>(1, std::min(div_up(dim, 256), most));
+    const dim3 joins((unsigned)heads, (unsigned)(wide + std::max<int64_t>(1, std::min(div_up(dim, 64), most))));
 #define AP_RUNS(A, B) hipLaunchKernelGGL((k_embed_grad_runs<A, B>), grid, dim3(256), 0, st, p, s, sl)
     AP_TYPES(dtype, table_dtype, AP_RUNS);
 #undef AP_RUNS
-    if (table_dtype == AP_F32) hipLaunchKernelGGL((k_embed_grad_join<AP_F32>), joins, dim3(256), 0, st, p, s, ws.runs);
-    else hipLaunchKernelGGL((k_embed_grad_join<AP_BF16>), joins, dim3(256), 0, st, p, s, ws.runs);
+    if (table_dtype == AP_F32) hipLaunchKernelGGL((k_embed_grad_join<AP_F32>), joins, dim3(256), 0, st, p, s, wide);
+    else hipLaunchKernelGGL((k_embed_grad_join<AP_BF16>), joins, dim3(256), 0, st, p, s, wide);
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }

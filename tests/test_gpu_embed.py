@@ -117,6 +117,21 @@ def test_gradient_of_many_tokens(vocab, n, dim):
     near(got, want, size, n, F32)
 
 
+@pytest.mark.parametrize("counts,dim,table_dtype", [
+    ([64, 128, 64 * 16, 64 * 17, 64 * 18, 63, 1, 65], 72, F32),           # tokens that end with a run, of up to and over 16 runs
+    ([1, 64 * 17 - 1, 64 * 17, 64 * 17 + 1, 2, 64 * 40 + 5], 520, BF16),
+    ([30_000] * 10 + [3] * 100, 8, F32)])                                  # longer blocks of the sort
+def test_gradient_of_tokens_over_many_runs(counts, dim, table_dtype):
+    rng = np.random.default_rng(len(counts))
+    tokens = np.repeat(np.arange(len(counts), dtype=np.int32), counts)
+    tokens = torch.from_numpy(rng.permutation(tokens))
+    grad = matrix(rng, len(tokens), dim, F32)
+    got = B.embed_grad(grad, tokens.to(DEV), len(counts) + 2, scale=2.0, dtype=table_dtype)
+    _, (want, size), _ = plain(torch.zeros((len(counts) + 2, dim)), None, tokens, None, 2.0, grad)
+    near(got, want, size, max(counts), table_dtype)
+    assert torch.equal(got, B.embed_grad(grad, tokens.to(DEV), len(counts) + 2, scale=2.0, dtype=table_dtype))
+
+
 @pytest.mark.parametrize("dtype,grad_dtype,dim,stride", [(F32, F32, 4, 0), (F32, F32, 260, 4), (BF16, BF16, 264, 8), (F32, BF16, 1000, 0), (BF16, F32, 2048, 0)])
 def test_gradient_of_the_weights(dtype, grad_dtype, dim, stride):
     rng = np.random.default_rng(dim)
