@@ -68,6 +68,12 @@ __device__ __forceinline__ void ap_g_load_lds(const char *base, uint32_t off, ui
     const ap_g_i32x4 rsrc = {(int32_t)(uint32_t)b, (int32_t)(uint32_t)(b >> 32), 0x7fffffff, 0x00020000};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory", "m0");
 }
+// 4 bytes a lane, likewise.
+__device__ __forceinline__ void ap_g_load_lds4(const void *base, uint32_t off, uint32_t lds) {
+    const uint64_t b = (uint64_t)base;
+    const ap_g_i32x4 rsrc = {(int32_t)(uint32_t)b, (int32_t)(uint32_t)(b >> 32), 0x7fffffff, 0x00020000};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory", "m0");
+}
 template <int N> __device__ __forceinline__ void ap_g_wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ap_g_barrier() {
     asm volatile("" ::: "memory");
@@ -75,9 +81,10 @@ __device__ __forceinline__ void ap_g_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// A tile of TM x TN by WM x WN waves.
-// A tile of TM x TN by WM x WN waves.
-template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> struct ApGemm {
+// A tile of TM x TN by WM x WN waves.  B_WIDE: a lane's columns lie next to each other, so that 16 lanes hold FB x 16 columns of a row in their order and
+// write them as whole lines (8-bit scores, 256 bytes a row past the caches: 5.3 TB/s, with 64 bytes at a time 3.0); B's rows are placed in LDS so.
+template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE, bool B_WIDE = false> struct ApGemm {
+    static_assert(B_LINE || !B_WIDE, "lines of columns stay in their order");
     static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
     static constexpr int FA = TM / WM / 16, FB = TN / WN / 16;   // 16 x 16 blocks of a wave
     static constexpr int A_BYTES = TM * AP_G_LINE, B_BYTES = TN * AP_G_LINE;
@@ -96,13 +103,13 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
     }
 
     // The offsets, relative to a chunk's first byte, of what this lane brings of an operand of T rows.
-    template <int T, bool LINE>
+    template <int T, bool LINE, bool WIDE = false>
     static __device__ __forceinline__ void offsets(const ApOperand &o, int wave, int lane, uint32_t (&off)[T / 8 / WAVES]) {
 #pragma unroll
         for (int i = 0; i < T / 8 / WAVES; i++) {
             const int at = (wave * (T / 8 / WAVES) + i) * 64 + lane;   // 16-byte group of the stage
             if (LINE) {
-                const int row = at >> 3, chunk = (at & 7) ^ swap_k(row);
+                const int line = at >> 3, chunk = (at & 7) ^ swap_k(line), row = WIDE ? (line & ~(16 * FB - 1)) + (line & 15) * FB + (line >> 4) % FB : line;
                 off[i] = row < o.rows ? (uint32_t)(row * o.ld + chunk * 16) : 0x80000000u;
             } else {
                 constexpr int PER = T * OP::BYTES / 16;   // groups of a line
@@ -157,22 +164,36 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
     // product takes `parts` = 3 pairs: second times first, first times second, first times first (the smallest first; the product
     // of the second parts is below the last bit of the sum).  2: only one operand has a second part, and the other's `.._part` is 0.
     static __device__ __forceinline__ void product(const ApOperand &A, const ApOperand &B, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB]) {
+        run<false>([&](int32_t, ApOperand &a, ApOperand &b) { a = A; b = B; }, 1, K, parts, a_part, b_part, lds, acc, [](int32_t) { return false; });
+    }
+    // The products of tiles 0 .. count - 1, one after the other without a pause: while a tile is finished the next one's first chunks come, so both
+    // stages stay in use.  tile_of(i, a, b) sets the operands of a tile, up to three tiles ahead, and may bring more into LDS for it; done(i) takes acc and says whether it has issued 56 stores or more, behind
+    // which the loads of the next chunk need not be waited for (memory operations of a wave end in their order).
+    template <class T, class D>
+    static __device__ __forceinline__ void products(T tile_of, int32_t count, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB], D done) {
+        run<true>(tile_of, count, K, parts, a_part, b_part, lds, acc, done);
+    }
+    template <bool MANY, class T, class D>
+    static __device__ __forceinline__ void run(T tile_of, int32_t count, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB], D done) {
         const int lane = threadIdx.x & 63, wave = ap_wave_id();
         const int wm = wave / WN, wn = wave % WN;
         uint32_t oa[TM / 8 / WAVES], ob[TN / 8 / WAVES];
+        ApOperand A, B;
+        tile_of(0, A, B);
         offsets<TM, A_LINE>(A, wave, lane, oa);
-        offsets<TN, B_LINE>(B, wave, lane, ob);
+        offsets<TN, B_LINE, B_WIDE>(B, wave, lane, ob);
+        auto clear = [&]() {
 #pragma unroll
-        for (int a = 0; a < FA; a++)
+            for (int i = 0; i < FA * FB; i++)
 #pragma unroll
-            for (int b = 0; b < FB; b++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) acc[a][b][r] = 0;
+                for (int r = 0; r < 4; r++) acc[i / FB][i % FB][r] = 0;
+        };
+        clear();
         const int32_t per = (K + BK - 1) / BK, chunks = per * parts;
         const int64_t a_step = A_LINE ? AP_G_LINE : BK * A.ld, b_step = B_LINE ? AP_G_LINE : BK * B.ld;
         const uint32_t lds0 = (uint32_t)(uintptr_t)(AP_LDS char *)lds;
         const char *next_a = A.base + (parts > 1 ? a_part : 0), *next_b = B.base;   // of the next chunk to be brought
-        int32_t left = K, part = 0;
+        int32_t left = K, part = 0, tile = 0;
         auto advance = [&]() {
             next_a += a_step;
             next_b += b_step;
@@ -180,7 +201,14 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
             if (left <= 0) {
                 part++;
                 left = part < parts ? K : 0;
-                next_a = A.base;
+                if (MANY && part == parts && ++tile < count) {
+                    tile_of(tile, A, B);
+                    offsets<TM, A_LINE>(A, wave, lane, oa);
+                    offsets<TN, B_LINE, B_WIDE>(B, wave, lane, ob);
+                    left = K;
+                    part = 0;
+                }
+                next_a = A.base + (MANY && part == 0 && parts > 1 ? a_part : 0);
                 next_b = B.base + (part == 1 ? b_part : 0);
             }
         };
@@ -208,7 +236,7 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
             bring(0);
             ap_g_wait_loads<0>();
             ap_g_barrier();
-            if (chunks > 1) bring(1);
+            if (MANY || chunks > 1) bring(1);
 #pragma unroll
             for (int b = 0; b < FB; b++) read_b(0, 0, b);
 #pragma unroll
@@ -219,8 +247,9 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
         if constexpr (OP::BYTES == 4)
 #pragma unroll
             for (int i = 0; i < NM; i++) total[i / FB][i % FB] = Acc{0, 0, 0, 0};
-        for (int32_t c = 0; c < chunks; c++) {
-            const int st = c & 1;
+        static_assert(!MANY || OP::BYTES != 4, "f32 sums are of one tile");
+        int32_t c = 0, st = 0, at = 0, behind_stores = 0;
+        while (MANY ? at < count : c < chunks) {
 #pragma unroll
             for (int i = 0; i < NM; i++) {
                 if (i < FB) read_b(st, 1, i);
@@ -230,7 +259,8 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
 #pragma unroll
             for (int i = 0; i < MEET; i++) mul(1, i);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            ap_g_wait_loads<0>();
+            if (MANY) asm volatile("s_waitcnt vmcnt(56)\n\ts_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:" ::"s"(behind_stores) : "memory", "scc");
+            else ap_g_wait_loads<0>();
             ap_g_barrier();
             // past the last chunk nothing is left: the loads bring zeros that nobody reads
             const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
@@ -253,6 +283,17 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
                 if ((c & 7) == 7 || c + 1 == chunks)
 #pragma unroll
                     for (int i = 0; i < NM; i++) { total[i / FB][i % FB] += acc[i / FB][i % FB]; acc[i / FB][i % FB] = Acc{0, 0, 0, 0}; }
+            st ^= 1;
+            c++;
+            if constexpr (MANY) {
+                behind_stores = 0;
+                if (c == chunks) {
+                    behind_stores = ap_uniform_i32(done(at));
+                    clear();
+                    c = 0;
+                    at++;
+                }
+            }
         }
         if constexpr (OP::BYTES == 4)
 #pragma unroll
@@ -262,7 +303,7 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE> st
     }
     // Where element r of this lane's block (a, b) lies: row(a) + r, col(b).
     static __device__ __forceinline__ int row(int a) { return ap_wave_id() / WN * (TM / WM) + a * 16 + 4 * ((threadIdx.x & 63) >> 4); }
-    static __device__ __forceinline__ int col(int b) { return ap_wave_id() % WN * (TN / WN) + b * 16 + (threadIdx.x & 15); }
+    static __device__ __forceinline__ int col(int b) { return ap_wave_id() % WN * (TN / WN) + (B_WIDE ? (threadIdx.x & 15) * FB + b : b * 16 + (threadIdx.x & 15)); }
     // Calls f(i, j, value) for every element that this lane holds of the tile.
     template <class F> static __device__ __forceinline__ void each(const Acc (&acc)[FA][FB], F f) {
 #pragma unroll

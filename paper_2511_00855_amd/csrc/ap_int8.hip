@@ -6,6 +6,7 @@
 // Few queries are bound by the documents' bytes: one pass (ap_stream.hpp), the queries rounded by every workgroup for itself.  Many
 // are bound by the f32 scores that are written (4 bytes for 2 dim operations) as much as by the matrix instruction.
 #include <algorithm>
+#include <type_traits>
 #include "ap_gemm.hpp"
 #include "ap_stream.hpp"
 
@@ -109,14 +110,50 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) 
                               });
 }
 
-// Queries are the product's rows: a lane then holds one document, and 32 lanes write 128 bytes of a query's scores, however they are aligned.
+// ROWS rows of a tile's scores, `docs` of TN columns each, from LDS to rows of memory that begin anywhere: whole lines past the caches, the ends with
+// them.  All are read before any is written, and lanes without a place write past the end of a buffer, which the hardware drops: conditions around the
+// reads and writes made the whole product 15 % longer.
+template <int TN, int ROWS, class L, class T>
+__device__ __forceinline__ void put_lines(int32_t docs, L from /* row -> const float * in LDS */, T to_of /* row -> float *, NULL for none */) {
+    typedef int32_t I4 __attribute__((ext_vector_type(4)));
+    typedef int32_t I4a __attribute__((ext_vector_type(4), aligned(4)));
+    constexpr uint32_t NONE = 0x80000000u;
+    constexpr int PAST = 2;   // nontemporal
+    const int lane = threadIdx.x & 63;
+    I4 v[ROWS];
+    int32_t end[ROWS];
+    uint32_t at[ROWS], at_end[ROWS];
+    float *to[ROWS];
+#pragma unroll
+    for (int j = 0; j < ROWS; j++) {
+        to[j] = reinterpret_cast<float *>(ap_uniform_u64((uint64_t)to_of(j)));
+        const int have = to[j] ? docs : 0, before = (int)(((uintptr_t)to[j] >> 2) & 31);   // floats of the first line that are not this tile's
+        const int first = (32 - before) & 31, last = ((have + before) & ~31) - before;      // columns of the whole lines: first .. last - 1
+        const int col = first + lane * 4, edge = lane < 32 ? lane : max(first, last) + lane - 32;   // lanes 0 to 31 what comes before, the others what is left
+        at[j] = col < last ? (uint32_t)col * 4 : NONE;
+        at_end[j] = edge < (lane < 32 ? min(first, have) : have) ? (uint32_t)edge * 4 : NONE;
+        const int32_t *row = reinterpret_cast<const int32_t *>(from(j));
+        v[j] = *reinterpret_cast<const I4a *>(row + min(col, TN - 4));   // whole lines end before TN
+        end[j] = row[edge & (TN - 1)];
+    }
+#pragma unroll
+    for (int j = 0; j < ROWS; j++) {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(to[j], 0, 0x7fffffff, 0x00020000);
+        __builtin_amdgcn_raw_buffer_store_b128(v[j], r, at[j], 0, PAST);
+        __builtin_amdgcn_raw_buffer_store_b32(end[j], r, at_end[j], 0, 0);
+    }
+}
+
+// Queries are the product's rows and a lane's documents lie together (B_WIDE): 16 lanes write 256 bytes of a query's scores.  Tiles of 128 and 64, for products
+// of which larger ones would leave compute units idle.
 template <int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64) void k_scores8(ApScores8 p) {
-    using G = ApGemm<ApI8Op, TM, TN, WM, WN, true, true>;
+    using G = ApGemm<ApI8Op, TM, TN, WM, WN, true, true, true>;
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS_BYTES];
     uint32_t nt, mt;
     ap_g_tile(blockIdx.x, (p.n + TN - 1) / TN, (p.rows + TM - 1) / TM, p.group, &nt, &mt);
     const int32_t m0 = mt * TM, n0 = nt * TN, queries = min(TM, p.rows - m0), docs = min(TN, p.n - n0);
+    typedef float Out __attribute__((ext_vector_type(G::FB), aligned(4)));   // a lane's scores of a row
     typename G::Acc acc[G::FA][G::FB];
     G::product({p.x + m0 * p.ldx, p.ldx, queries}, {p.q + n0 * p.ldq, p.ldq, docs}, p.pad, 1, 0, 0, lds, acc);
     // all scales first: a load between the stores would wait for them
@@ -127,18 +164,17 @@ __global__ __launch_bounds__(WM *WN * 64) void k_scores8(ApScores8 p) {
     for (int a = 0; a < G::FA; a++)
 #pragma unroll
         for (int r = 0; r < 4; r++) sx[a][r] = p.x_scale[m0 + min(G::row(a) + r, queries - 1)];
-    // Past the caches: the scores would push out the rows that the next tiles read (10,000 x 100,000 of 768 columns: 1.48 -> 1.03 ms).  Stores past the
-    // caches are fast for whole 64 bytes only.  Where rows begin anywhere (100,011 documents: 1.77 ms), the tile goes through LDS and
-    // leaves in the lines of memory, with the caches to join the ends of its rows with its neighbours' (1.49 ms).
+    // past the caches: the scores would push out the rows that the next tiles read
     float *out = p.out + (int64_t)m0 * p.ld_out + n0;
     if (queries == TM && docs == TN && (((uintptr_t)p.out | p.ld_out * 4) & 63) == 0) {
 #pragma unroll
         for (int a = 0; a < G::FA; a++)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-                float *to = out + (G::row(a) + r) * p.ld_out;
+                Out v;
 #pragma unroll
-                for (int b = 0; b < G::FB; b++) __builtin_nontemporal_store((float)acc[a][b][r] * sx[a][r] * sd[b], to + G::col(b));
+                for (int b = 0; b < G::FB; b++) v[b] = (float)acc[a][b][r] * sx[a][r] * sd[b];
+                __builtin_nontemporal_store(v, reinterpret_cast<Out *>(out + (G::row(a) + r) * p.ld_out + G::col(0)));
             }
         return;
     }
@@ -149,34 +185,116 @@ __global__ __launch_bounds__(WM *WN * 64) void k_scores8(ApScores8 p) {
 #pragma unroll
         for (int a = 0; a < FP; a++)
 #pragma unroll
-            for (int b = 0; b < G::FB; b++)
+            for (int r = 0; r < 4; r++) {
+                const int row = wave / WN * WR + a * 16 + 4 * (lane >> 4) + r;
+                Out v;
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const int row = wave / WN * WR + a * 16 + 4 * (lane >> 4) + r;   // 4 rows at a time in four different parts of the banks
-                    *reinterpret_cast<float *>(lds + row * LINE + ((G::col(b) * 4) ^ ((row >> 2 & 3) << 6))) = (float)acc[h * FP + a][b][r] * sx[h * FP + a][r] * sd[b];
-                }
-        __syncthreads();
-        for (int row = wave; row < WM * WR; row += G::WAVES) {
-            const int i = row / WR * (TM / WM) + h * WR + row % WR;
-            if (i >= queries) continue;
-            float *to = out + i * p.ld_out;
-            const int before = (int)(((uintptr_t)to >> 2) & 31);   // floats of the first line that are not this tile's
-            auto at = [&](int col) { return *reinterpret_cast<const float *>(lds + row * LINE + ((col * 4) ^ ((row >> 2 & 3) << 6))); };
-            const int first = (32 - before) & 31, last = ((docs + before) & ~31) - before;   // columns of the whole lines: first .. last - 1
-#pragma unroll
-            for (int k = 0; k < TN; k += 64) {
-                const int col = first + k + lane;
-                if (col < last) __builtin_nontemporal_store(at(col & (TN - 1)), to + col);
+                for (int b = 0; b < G::FB; b++) v[b] = (float)acc[h * FP + a][b][r] * sx[h * FP + a][r] * sd[b];
+                *reinterpret_cast<Out *>(lds + row * LINE + G::col(0) * 4) = v;
             }
-            // lanes 0 to 31 what comes before, the others what is left
-            const int col = lane < 32 ? lane : max(first, last) + lane - 32;
-            if (lane < 32 ? col < min(first, docs) : col < docs) to[col] = at(col);
-        }
+        __syncthreads();
+        for (int row = wave * 2; row < WM * WR; row += G::WAVES * 2)
+            put_lines<TN, 2>(docs, [&](int j) { return reinterpret_cast<const float *>(lds + (row + j) * LINE); }, [&](int j) {
+                const int k = row + j, i = k / WR * (TM / WM) + h * WR + k % WR;
+                return i < queries ? out + i * p.ld_out : nullptr;
+            });
         __syncthreads();
     }
 }
 
+// The largest tiles: a workgroup takes every gridDim.x-th, and its scores leave while the next tile is multiplied.  The stores bound the short rows, the matrix
+// instruction with the card's power the long ones: 8,192 queries over 100,096 documents take 625 us with 128 columns (5.2 TB/s written), 10,000 over
+// 100,000 with 768 1,070 us (1,430 TOP/s, 3.7 TB/s; a tile a workgroup 1,240, and with 64 bytes of a row at a time 1,260).  LINES: rows of scores begin
+// anywhere.  16 rows at a time then go through LDS, so that what leaves past the caches is whole lines of memory: over 100,011 documents 700 us with 128
+// columns (past the caches from the registers 1,430, with them 940) and 1,480 with 768.
+template <int TM, int TN, int WM, int WN, bool LINES>
+__global__ __launch_bounds__(WM *WN * 64) void k_scores8_many(ApScores8 p) {
+    using G = ApGemm<ApI8Op, TM, TN, WM, WN, true, true, true>;
+    static_assert(TM == 256 && TN == 256 && G::WAVES == 8, "a wave brings 64 scales");
+    __shared__ __attribute__((aligned(1024))) char lds[G::LDS_BYTES];
+    __shared__ __attribute__((aligned(16))) float s_rows[LINES ? 16 : 1][TN];
+    __shared__ __attribute__((aligned(16))) float s_scale[4][2][256];   // of four tiles: the queries', the documents'
+    const int lane = threadIdx.x & 63, wave = ap_wave_id();
+    const uint32_t nts = (p.n + TN - 1) / TN, mts = (p.rows + TM - 1) / TM;
+    auto place = [&](int32_t i, int32_t *m0, int32_t *n0) {
+        uint32_t nt, mt;
+        ap_g_tile(blockIdx.x + i * gridDim.x, nts, mts, p.group, &nt, &mt);
+        *m0 = mt * TM;
+        *n0 = nt * TN;
+    };
+    typedef float Out __attribute__((ext_vector_type(G::FB), aligned(4)));
+    typename G::Acc acc[G::FA][G::FB];
+    auto lds_barrier = []() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); ap_g_barrier(); };   // stores are not waited for
+    auto tile_of = [&](int32_t i, ApOperand &a, ApOperand &b) {
+        int32_t m0, n0;
+        place(i, &m0, &n0);
+        a = ApOperand{p.x + m0 * p.ldx, p.ldx, min(TM, p.rows - m0)};
+        b = ApOperand{p.q + n0 * p.ldq, p.ldq, min(TN, p.n - n0)};
+        const int k = wave % 4 * 64;
+        const uint64_t from = ap_uniform_u64((uint64_t)(wave < 4 ? p.x_scale + m0 : p.q_scale + n0));
+        ap_g_load_lds4(reinterpret_cast<const void *>(from), k + lane < (wave < 4 ? a.rows : b.rows) ? (uint32_t)(k + lane) * 4 : 0x80000000u,
+                       ap_uniform_i32((uint32_t)(uintptr_t)(AP_LDS float *)&s_scale[i & 3][wave / 4][k]));
+    };
+    auto done = [&](int32_t i) {
+        int32_t m0, n0;
+        place(i, &m0, &n0);
+        const int32_t queries = min(TM, p.rows - m0), docs = min(TN, p.n - n0);
+        float sd[G::FB];
+#pragma unroll
+        for (int b = 0; b < G::FB; b++) sd[b] = s_scale[i & 3][1][G::col(b)];
+        const bool whole = queries == TM && docs == TN;
+        float *out = p.out + (int64_t)m0 * p.ld_out + n0;
+        if constexpr (LINES) {
+#pragma unroll
+            for (int a = 0; a < G::FA; a++) {
+                const float4 s = *reinterpret_cast<const float4 *>(&s_scale[i & 3][0][G::row(a)]);
+                const float sx[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                for (int h = 0; h < 4; h += 2) {
+#pragma unroll
+                    for (int r = h; r < h + 2; r++) {
+                        Out v;
+#pragma unroll
+                        for (int b = 0; b < G::FB; b++) v[b] = (float)acc[a][b][r] * sx[r] * sd[b];
+                        *reinterpret_cast<Out *>(&s_rows[wave / WN * 8 + (lane >> 4) * 2 + r - h][G::col(0)]) = v;
+                    }
+                    lds_barrier();
+                    put_lines<TN, 2>(docs, [&](int j) { return s_rows[wave * 2 + j]; }, [&](int j) {
+                        const int k = wave * 2 + j, row = k / 8 * (TM / WM) + a * 16 + k % 8 / 2 * 4 + h + j;
+                        return row < queries ? out + row * p.ld_out : nullptr;
+                    });
+                    lds_barrier();
+                }
+            }
+            return false;
+        }
+        auto put = [&](auto all) {
+#pragma unroll
+            for (int a = 0; a < G::FA; a++) {
+                const float4 s = *reinterpret_cast<const float4 *>(&s_scale[i & 3][0][G::row(a)]);
+                const float sx[4] = {s.x, s.y, s.z, s.w};
+                float *to = out + G::row(a) * p.ld_out + G::col(0);
+#pragma unroll
+                for (int r = 0; r < 4; r++, to += p.ld_out) {
+                    Out v;
+#pragma unroll
+                    for (int b = 0; b < G::FB; b++) v[b] = (float)acc[a][b][r] * sx[r] * sd[b];
+                    if (decltype(all)::value) __builtin_nontemporal_store(v, reinterpret_cast<Out *>(to));
+                    else if (G::row(a) + r < queries)
+#pragma unroll
+                        for (int b = 0; b < G::FB; b++)
+                            if (G::col(b) < docs) to[b] = v[b];
+                }
+            }
+        };
+        if (whole) put(std::true_type{}); else put(std::false_type{});
+        return false;
+    };
+    G::products(tile_of, (int32_t)((nts * mts - blockIdx.x + gridDim.x - 1) / gridDim.x), p.pad, 1, 0, 0, lds, acc, done);
+}
+
 // ------------------------------------------------------------------ host side
+#define AP_CUS 256
 static int64_t div_up(int64_t v, int64_t m) { return (v + m - 1) / m; }
 static int check_dim(int32_t dim, int32_t dtype) {
     AP_REQUIRE(dtype == AP_F32 || dtype == AP_BF16 || dtype == AP_I8, "dtype = %d is not AP_F32/AP_BF16/AP_I8", dtype);
@@ -267,7 +385,10 @@ extern "C" int ap_scores_int8(const void *x, int64_t ldx, const float *x_scale, 
     AP_REQUIRE(tiles < (1ll << 31) / 512, "rows x n is too large");
     p.group = (int32_t)std::min<int64_t>(div_up(rows, tile), 8);
     const dim3 grid((unsigned)tiles);
-    if (tile == 256) hipLaunchKernelGGL((k_scores8<256, 256, 2, 4>), grid, dim3(512), 0, st, p);
+    const dim3 many(std::min<unsigned>(grid.x, AP_CUS));
+    const bool lines = ((((uintptr_t)p.out) | (uintptr_t)(p.ld_out * 4)) & 63) != 0;
+    if (tile == 256 && lines) hipLaunchKernelGGL((k_scores8_many<256, 256, 2, 4, true>), many, dim3(512), 0, st, p);
+    else if (tile == 256) hipLaunchKernelGGL((k_scores8_many<256, 256, 2, 4, false>), many, dim3(512), 0, st, p);
     else if (tile == 128) hipLaunchKernelGGL((k_scores8<128, 128, 2, 2>), grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((k_scores8<64, 64, 2, 2>), grid, dim3(256), 0, st, p);
     AP_CHECK_HIP(hipGetLastError());
