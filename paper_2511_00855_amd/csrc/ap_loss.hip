@@ -252,7 +252,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
     }
     if (GRAD) {
         // a part of the coefficients goes through LDS, a query's documents together, and leaves in whole lines (four documents of a lane at a time
-        // would write 32 bytes of 16 lines: a tile of 256 took half as long again); groups of 16 bytes change places by the query
+        // would write 32 bytes of 16 lines); groups of 16 bytes change places by the query
         constexpr int LINE = TM * OP::BYTES, GROUPS = LINE / 16;
         for (int part = 0; part < (p.c_part ? 2 : 1); part++) {
 #pragma unroll
@@ -283,6 +283,76 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
             p.part[(int64_t)mt * p.rows + n0 + col] = make_float2(m, s);
         }
     }
+}
+
+// The coefficients by tiles of 256, of which a workgroup takes every gridDim.x-th: while one's coefficients are made and leave, the next one's rows come.
+// Queries are the product's rows and a lane's documents lie together (B_WIDE): 16 lanes write a line of a query's coefficients.  4,096 queries over 16,128
+// bf16 rows of 1,024: 132 us (1,020 TFLOP/s), a tile a workgroup and lines through LDS 144; 2,048 over 32,768 f32 rows of 768 in parts: 310 and 369 us.
+// The loss's own tiles gain nothing by it: 229 and 230 us for 1,000 over 120,011; there the exponentials, 5 us of a tile's 30, are all that stands
+// between two products.
+template <class OP, bool PARTS>
+__global__ __launch_bounds__(512) void k_loss_coefs(ApLoss p) {
+    using G = ApGemm<OP, 256, 256, 2, 4, true, true, true>;
+    constexpr int T = 256;
+    constexpr bool EXACT = !std::is_same<OP, ApBf16Op>::value;
+    __shared__ __attribute__((aligned(1024))) char lds[G::LDS_BYTES];
+    __shared__ __attribute__((aligned(16))) float s_of[4][3][T];   // of four tiles: the queries' lse, weights, labels
+    const int lane = threadIdx.x & 63, wave = ap_wave_id();
+    const uint32_t mts = (p.count + T - 1) / T, nts = (p.rows + T - 1) / T;
+    const ApFactor f(p.scale, PARTS ? p.amax : nullptr);
+    auto place = [&](int32_t i, int32_t *m0, int32_t *n0) {
+        uint32_t mt, nt;
+        ap_g_tile(blockIdx.x + i * gridDim.x, mts, nts, p.group, &mt, &nt);
+        *m0 = mt * T;
+        *n0 = nt * T;
+    };
+    typename G::Acc acc[G::FA][G::FB];
+    auto tile_of = [&](int32_t i, ApOperand &a, ApOperand &b) {
+        int32_t m0, n0;
+        place(i, &m0, &n0);
+        a = ApOperand{p.x + n0 * p.ldx, p.ldx, min(T, p.rows - n0)};
+        b = ApOperand{p.docs + (p.first + m0) * p.ldd, p.ldd, min(T, p.count - m0)};
+        const int k = wave % 4 * 64 + lane;
+        const uint32_t off = k < a.rows ? (uint32_t)k * 4 : 0x80000000u;   // of a query that is not there: zeros
+        auto to = [&](int what) { return (uint32_t)ap_uniform_i32((int32_t)(uint32_t)(uintptr_t)(AP_LDS float *)&s_of[i & 3][what][wave % 4 * 64]); };
+        ap_g_load_lds4(reinterpret_cast<const void *>(ap_uniform_u64((uint64_t)((wave < 4 ? p.lse : p.coef) + n0))), off, to(wave / 4));
+        if (wave < 4) ap_g_load_lds4(p.labels + n0, off, to(2));
+    };
+    auto done = [&](int32_t i) {
+        int32_t m0, n0;
+        place(i, &m0, &n0);
+        const int32_t docs = min(T, p.count - m0), queries = min(T, p.rows - n0), col0 = G::col(0);
+        const int32_t before = (int32_t)p.first + m0 + col0;   // this lane's first document
+        char *out = p.c + (int64_t)n0 * p.ldc + (int64_t)(m0 + col0) * OP::BYTES;
+#pragma unroll
+        for (int a = 0; a < G::FA; a++) {
+            const int row = G::row(a);
+            const float4 l4 = *reinterpret_cast<const float4 *>(&s_of[i & 3][0][row]), g4 = *reinterpret_cast<const float4 *>(&s_of[i & 3][1][row]);
+            const int4 t4 = *reinterpret_cast<const int4 *>(&s_of[i & 3][2][row]);
+            const float l[4] = {l4.x, l4.y, l4.z, l4.w}, g[4] = {g4.x, g4.y, g4.z, g4.w};
+            const int32_t t[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                const ApCoef coef(g[r], l[r]);
+                float v[4];
+#pragma unroll
+                for (int b = 0; b < 4; b++) {
+                    const float e = coef.template exp_of<PARTS, EXACT>(acc[a][b][r], f);
+                    v[b] = coef.times((uint32_t)t[r] - (uint32_t)before == (uint32_t)b ? e - 1.f : e);
+                    if (col0 + b >= docs) v[b] = 0.f;
+                }
+                char *to = out + (row + r) * p.ldc;
+                const uint2 first = ap_coef_part<PARTS>(v);
+                if (row + r < queries) *reinterpret_cast<uint2 *>(to) = first;
+                if (PARTS || p.c_part) {
+                    const uint2 second = ap_coef_part<PARTS>(v);
+                    if (row + r < queries) *reinterpret_cast<uint2 *>(to + p.c_part) = second;
+                }
+            }
+        }
+        return false;
+    };
+    G::products(tile_of, (int32_t)((mts * nts - blockIdx.x + gridDim.x - 1) / gridDim.x), p.dim, PARTS ? 3 : 1, p.x_part, p.d_part, lds, acc, done);
 }
 
 // Joins the (maximum, sum) pairs of a query.  1,024 threads take 2^qb queries; the pairs of a query are shared out to 1024 / 2^qb threads
@@ -702,6 +772,7 @@ __global__ __launch_bounds__(512) void k_loss_few_grads(ApLossFew p) {
 
 // ------------------------------------------------------------------ host side
 static int64_t up_to(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+#define AP_CUS 256   // compute units
 static int64_t div_up(int64_t v, int64_t m) { return (v + m - 1) / m; }
 
 // The workspace of one call: arrays one after the other, each at a multiple of 256 bytes.  Without a base it is only measured.
@@ -795,7 +866,10 @@ static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
     const dim3 grid((unsigned)(mt * nt));
     p.group = (int32_t)std::min<int64_t>(nt, 8);
     if (tile == 256) {
-        if constexpr (OP::BYTES == 2) hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
+        if constexpr (OP::BYTES == 2) {
+            if constexpr (GRAD) hipLaunchKernelGGL((k_loss_coefs<OP, PARTS>), dim3(std::min<unsigned>(grid.x, AP_CUS)), dim3(512), 0, st, p);
+            else hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
+        }
     } else if (tile == 128) hipLaunchKernelGGL((k_loss_tiles<OP, 128, 128, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((k_loss_tiles<OP, 64, 64, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
     AP_CHECK_HIP(hipGetLastError());
