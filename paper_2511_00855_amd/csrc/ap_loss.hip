@@ -32,7 +32,8 @@ __device__ __forceinline__ void ap_load4(const ApSide &s, int32_t per, int64_t t
         if (at < total) v[k] = *reinterpret_cast<const float4 *>(s.p + (s.ld == per * 4 ? at * 4 : at / per * s.ld + at % per * 4));
     }
 }
-// Largest finite magnitude of two arrays, a number of every workgroup: the bits of a float, which are in the order of the numbers.
+// Largest finite magnitude of two arrays, a number of every workgroup: the bits of a float, which are in the order of the numbers.  Bound by its loads:
+// 100,000 rows of 768 take 55 us (5.6 TB/s).
 #define AP_LOSS_AMAX 2048
 __global__ __launch_bounds__(256) void k_loss_amax(ApSide a, ApSide b, int32_t dim, uint32_t *__restrict__ out /* [2][gridDim.x] */) {
     __shared__ float s_m[4];
@@ -63,6 +64,7 @@ __device__ __forceinline__ int ap_loss_up(uint32_t amax) { return amax ? 14 - il
 
 // Rows in two f16 parts, `pad` columns each (zeros after the last).  The first `blocks_a` workgroups take the documents, the others the queries; queries
 // that `coef` gives 0 become zeros.  amax: the numbers of k_loss_amax, `parts` of each side; their maxima go to `both`.
+// Bound by memory: 100,000 rows of 768, 307 MB in and as much out, take 113 us (5.5 TB/s).
 __global__ __launch_bounds__(256) void k_loss_split(ApSide a, ApSide b, int32_t blocks_a, int32_t dim, int32_t pad, const uint32_t *__restrict__ amax, int32_t parts, uint32_t *__restrict__ both,
                                                     const float *__restrict__ coef, _Float16 *__restrict__ out_a, _Float16 *__restrict__ out_b) {
     __shared__ uint32_t s_m[4];
@@ -174,7 +176,9 @@ template <bool F16> __device__ __forceinline__ uint2 ap_coef_part(float (&v)[4])
     return h;
 }
 
-// GRAD: the tile's coefficients.  Otherwise its maximum and sum a query.
+// GRAD: the tile's coefficients (tiles of 128 and 64; k_loss_coefs has the largest).  Otherwise its maximum and sum a query.  Bound by the matrix
+// instruction and the card's power: 4,096 queries over 250,002 bf16 rows of 1,024 take 1,860 us (1,130 TFLOP/s), 2,048 over 100,000 f32 rows of 768 in
+// parts 870 us (1,085 of f16 products); 100 over 2,000 f32 rows of 128 take 7 us, and there a launch is most of it.
 template <class OP, int TM, int TN, int WM, int WN, bool PARTS, bool GRAD>
 __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
     using G = ApGemm<OP, TM, TN, WM, WN, true, true>;
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(512) void k_loss_coefs(ApLoss p) {
 }
 
 // Joins the (maximum, sum) pairs of a query.  1,024 threads take 2^qb queries; the pairs of a query are shared out to 1024 / 2^qb threads
-// and joined in a fixed tree.
+// and joined in a fixed tree.  Waits for memory: 5 us for 1,000 queries of 469 pairs, 9 us for 4,096 of 977.
 __global__ __launch_bounds__(1024) void k_loss_join(const float2 *__restrict__ part, int64_t tiles, int32_t rows, int qb, const int32_t *__restrict__ labels, int32_t n,
                                                     const float *__restrict__ at_label, float scale, const uint32_t *__restrict__ amax, float *__restrict__ loss, float *__restrict__ lse) {
     const ApFactor f(scale, amax);
@@ -393,7 +397,8 @@ __global__ __launch_bounds__(1024) void k_loss_join(const float2 *__restrict__ p
 }
 
 // Few queries: one pass over the documents as they are (f32 rows by the f32 instruction: memory is slower).  A lane has one query and four
-// documents at a time; a workgroup leaves one pair of every query behind.
+// documents at a time; a workgroup leaves one pair of every query behind.  Bound by its loads: 100,000 f32 rows of 768 take 58 us (5.3 TB/s) for one
+// query, 120,011 bf16 rows of 1,024 43 to 46 us for 1 to 64 (5.5 TB/s).
 template <int DT, int NQ, bool GRAD>
 __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -483,7 +488,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_loss_few(ApLoss p) {
 // *most = the largest |g_q| of the queries that have a label (1 if there is none): the coefficients are stored relative to it, so that equal weights
 // leave the label's own coefficient p - 1 without a rounding of the weight.  coef[q] = g_q / *most, 0 without a label.  With `out`, the queries too
 // (groups of 16 bytes), zeros for those of coefficient 0: what is multiplied by 0 must not be infinite or NaN.  Every workgroup finds the largest
-// by itself (up to AP_LOSS_PREP queries), or is told (`given`).
+// by itself (up to AP_LOSS_PREP queries), or is told (`given`).  5 to 8 us, a launch and three waits.
 #define AP_LOSS_PREP 16384
 __global__ __launch_bounds__(1024) void k_loss_prep(const float *__restrict__ g, const int32_t *__restrict__ labels, int32_t rows, int32_t n, const float *__restrict__ given,
                                                     float *__restrict__ most, float *__restrict__ coef, const char *__restrict__ x, int64_t ld, int32_t groups, uint4 *__restrict__ out) {
@@ -530,6 +535,9 @@ struct ApLossGrad {
     int32_t start;                 // 1: first piece, nothing is there to add to
 };
 
+// A piece's share of both gradients out of its coefficients: the first workgroups take the queries' (runs of the documents), the others the documents'.
+// Bound by the matrix instruction and the card's power: 4,096 queries x 16,128 documents x 1,024 in bf16 take 211 us (1,280 TFLOP/s), 2,048 x 32,768 x 768 in
+// parts 545 us (1,135 of f16 products).
 template <class OP, int TM, int TN, int WM, int WN, bool PARTS>
 __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
     constexpr int SIZE = OP::BYTES;
@@ -590,7 +598,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
     }
 }
 
-// The sums of many runs: 16 threads share an element's.
+// The sums of many runs: 16 threads share an element's, or one query's few elements would wait for hundreds of loads in turn.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_loss_gx_many(const float *__restrict__ gx, int32_t runs, int64_t total, float scale, const float *__restrict__ most, void *__restrict__ out) {
     __shared__ float4 s_sum[16][16];
@@ -612,6 +620,7 @@ __global__ __launch_bounds__(256) void k_loss_gx_many(const float *__restrict__ 
     if (BF16) reinterpret_cast<uint2 *>(out)[i] = make_uint2(ap_bf16_pair(s.x, s.y), ap_bf16_pair(s.z, s.w));
     else reinterpret_cast<float4 *>(out)[i] = s;
 }
+// The sums of few runs.  5 to 10 us.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, int32_t splits, int32_t rows, int32_t dim, float scale, const float *__restrict__ most,
                                                  const uint32_t *__restrict__ amax, void *__restrict__ out, int64_t ld) {
@@ -635,6 +644,8 @@ __global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, i
 // has NB blocks of 16 columns: VEC values of a lane's load belong to as many blocks, so that block t is made of the columns VEC n + t and
 // loads and stores are whole lines.  16 documents at a time: their rows times the coefficients go to sums of the queries' gradient that stay
 // in registers, the queries (in registers too) times the coefficients are the documents' gradient.
+// Bound by memory up to 16 queries, every byte once in and once out: 120,011 bf16 rows of 1,024 121 us for one (4.1 TB/s), 100,000 f32 rows of 768 131 us for
+// 16 (4.7 TB/s); by the f32 instruction above: 172 us for 32 bf16 queries, 250 for 64 of f32.
 struct ApLossFew {
     const char *docs, *x;          // x: without queries of weight 0
     int64_t ldd, ldx;
@@ -878,8 +889,9 @@ static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
 
 template <int DT, bool GRAD> static int launch_few(const ApLoss &all, hipStream_t st) {
     const int64_t row_bytes = (int64_t)all.dim * (DT == AP_F32 ? 4 : 2), blocks = ap_stream_blocks(all.count);
-    const int32_t group = few_group(row_bytes);
-    for (int32_t q0 = 0; q0 < all.rows; q0 += group) {   // as many queries at a time as LDS holds
+    // as many passes as LDS makes it, of queries shared out evenly: 64 over 100,000 f32 rows of 768 take two of 32, 162 us, 48 and 16 165
+    const int32_t passes = (int32_t)div_up(all.rows, few_group(row_bytes)), group = (int32_t)div_up(div_up(all.rows, passes), 16) * 16;
+    for (int32_t q0 = 0; q0 < all.rows; q0 += group) {
         ApLoss p = all;
         p.all = all.rows;
         p.rows = std::min(group, all.rows - q0);
