@@ -183,11 +183,25 @@ __global__ __launch_bounds__(256) void k_embed_zero_unnamed(char *__restrict__ o
 }
 
 // The list that entry e lies in, -1 for none.
-__device__ __forceinline__ int64_t row_of(const int64_t *indptr, int64_t rows, int64_t e) {
+__device__ __forceinline__ int64_t row_of(const int64_t *indptr, int64_t rows, int64_t n, int64_t e) {
     if (!indptr) return e;
     int64_t lo = 0, hi = rows;   // indptr[lo] <= e, or lo = 0
     while (hi - lo > 1) { const int64_t m = (lo + hi) / 2; if (indptr[m] <= e) lo = m; else hi = m; }
-    return indptr[lo] <= e && e < indptr[lo + 1] ? lo : -1;
+    return indptr[lo] <= e && e < indptr[lo + 1] && ap_row_ok(indptr, lo, n) ? lo : -1;
+}
+// The same for a wave that has one entry: 64 offsets at a time.
+__device__ __forceinline__ int64_t wave_row_of(const int64_t *indptr, int64_t rows, int64_t n, int64_t e) {
+    if (!indptr) return e;
+    int64_t lo = 0, hi = rows;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, m = lo + (threadIdx.x & 63) * step;
+        const uint64_t past = ~__ballot(m < hi && (m == lo || indptr[m] <= e));
+        const int k = past ? __builtin_ctzll(past) : 64;   // the first k are not past the entry; the first of all never is
+        hi = min(hi, lo + k * step);
+        lo += (k - 1) * step;
+        if (step == 1) break;
+    }
+    return indptr[lo] <= e && e < indptr[lo + 1] && ap_row_ok(indptr, lo, n) ? lo : -1;
 }
 
 #define AP_EMBED_FEW 4096   // entries that find their equals by reading the list
@@ -244,7 +258,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
         const bool same = e + lane < end && p.tokens[e + lane] == t;
         const uint64_t m = __ballot(same);
         if (same) {
-            const int k = at + __popcll(m & ((1ull << lane) - 1)), row = (int)row_of(p.indptr, p.rows, e + lane);
+            const int k = at + __popcll(m & ((1ull << lane) - 1)), row = (int)row_of(p.indptr, p.rows, p.n, e + lane);
             s_row[k] = row;
             s_w[k] = row >= 0 ? p.scale * (p.weights ? p.weights[e + lane] : 1.f) : 0.f;
         }
@@ -580,7 +594,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(ApEmbed p, ApRuns s, in
 // out[slab][entry].  Bound by what the L2s gather: 1.2M entries of bf16 rows of 1,024 take 201 us (12.2 TB/s); eight loads ahead instead of four 233, as
 // fewer waves fit.
 template <int DT, int GT>
-__global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s, const int32_t *__restrict__ rows /* of every entry; NULL: looked up */, const char *__restrict__ g, int64_t ldg,
+__global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s, const int32_t *__restrict__ rows /* of every entry; NULL: itself */, const char *__restrict__ g, int64_t ldg,
                                                             float *__restrict__ out) {
     // 16 bytes of the wider type: four or eight columns a lane
     constexpr int N = DT == AP_BF16 && GT == AP_BF16 ? 8 : 4;
@@ -588,12 +602,12 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
     int64_t unit;
     if (!slab_block(s, &slab, &unit)) return;
     const int l16 = threadIdx.x & 15;
-    const int64_t e = unit * blockDim.x + threadIdx.x;   // this lane's entry
+    const int64_t e = unit * 256 + threadIdx.x;   // this lane's entry
     int32_t row = -1, tok = -1;
     if (e < p.n) {
         tok = p.tokens[e];
         if (tok >= p.vocab) tok = -1;
-        if (tok >= 0) row = rows ? rows[e] : (int32_t)row_of(p.indptr, p.rows, e);
+        if (tok >= 0) row = rows ? rows[e] : (int32_t)e;
     }
     const int32_t col = (slab * 16 + l16) * N;
     const bool mine = col < p.dim;
@@ -641,6 +655,43 @@ __global__ __launch_bounds__(256) void k_embed_grad_weights(ApEmbed p, ApSlabs s
         });
     });
     if (e < p.n) out[slab * p.n + e] = own * p.scale;
+}
+// Few entries: a wave takes an entry with all of its columns, one launch, where slabs take four (the list of every entry, which is two, and the sum of the
+// parts): 512 entries of f32 rows of 768 4 us and 9, 8,000 7 and 14, 40,000 23 and 23; 60,000 of bf16 rows of 1,024 35 and 34, 160,000 of f32 rows of
+// 128 66 and 21.
+#define AP_EMBED_FEW_WEIGHTS (1 << 15)
+template <int DT, int GT>
+__global__ __launch_bounds__(256) void k_embed_grad_weights_few(ApEmbed p, const char *__restrict__ g, int64_t ldg, float *__restrict__ out) {
+    constexpr int N = DT == AP_BF16 && GT == AP_BF16 ? 8 : 4;
+    const int lane = threadIdx.x & 63;
+    const int64_t e = blockIdx.x * (int64_t)4 + ap_wave_id();
+    if (e >= p.n) return;
+    const int32_t tok = p.tokens[e];
+    const int64_t row = tok >= 0 && tok < p.vocab ? wave_row_of(p.indptr, p.rows, p.n, e) : -1;
+    float sum = 0.f;
+    if (row >= 0)
+        for (int32_t c0 = lane * N; c0 < p.dim; c0 += 64 * N * 4) {
+            uint4 x[4], y[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int32_t c = c0 + 64 * N * k;
+                x[k] = y[k] = make_uint4(0, 0, 0, 0);
+                if (c >= p.dim) continue;
+                const char *a = p.table + tok * p.ld + c * (DT == AP_F32 ? 4 : 2), *b = g + row * ldg + c * (GT == AP_F32 ? 4 : 2);
+                if (DT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(a); x[k].x = v.x; x[k].y = v.y; } else x[k] = *reinterpret_cast<const uint4 *>(a);
+                if (GT == AP_BF16 && N == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(b); y[k].x = v.x; y[k].y = v.y; } else y[k] = *reinterpret_cast<const uint4 *>(b);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                float u[8], v[8];
+                ApRow16<DT>::get(x[k], u);
+                ApRow16<GT>::get(y[k], v);
+#pragma unroll
+                for (int j = 0; j < N; j++) sum = fmaf(u[j], v[j], sum);
+            }
+        }
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) out[e] = sum * p.scale;
 }
 // The slabs' parts of an entry.  1.2M entries of eight slabs: 9 us.
 __global__ __launch_bounds__(256) void k_embed_grad_weights_sum(const float *__restrict__ parts, int64_t n, int32_t slabs, float *__restrict__ out) {
@@ -815,8 +866,8 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
 // The workspace of the weights' gradient: the parts of each slab, and for many entries of lists the list of each.
 static void weights_layout(int64_t n, int32_t dim, int32_t dtype, int32_t grad_dtype, int32_t *slabs, size_t *parts, size_t *rows) {
     *slabs = (int32_t)div_up(dim, dtype == AP_BF16 && grad_dtype == AP_BF16 ? 128 : 64);
-    *parts = *slabs > 1 ? (size_t)div_up(n * *slabs * 4, 256) * 256 : 0;
-    *rows = n > AP_EMBED_FEW ? (size_t)n * 4 : 0;
+    *parts = *slabs > 1 && n > AP_EMBED_FEW_WEIGHTS ? (size_t)div_up(n * *slabs * 4, 256) * 256 : 0;
+    *rows = n > AP_EMBED_FEW_WEIGHTS ? (size_t)n * 4 : 0;
 }
 
 extern "C" int ap_embed_grad_weights_bytes(int64_t n, int32_t dim, int32_t dtype, int32_t grad_dtype, size_t *out) {
@@ -847,14 +898,19 @@ extern "C" int ap_embed_grad_weights(const void *grad_out, int64_t ldg, int32_t 
     const ApEmbed p = args_of(table, ld, dtype, vocab, dim, lists, scale, nullptr);
     const char *g = static_cast<const char *>(grad_out);
     const int64_t ldb = ldg * (grad_dtype == AP_BF16 ? 2 : 4);
-    const unsigned threads = lists->n > (1 << 14) ? 256 : 64;   // few entries: as many workgroups as there can be
-    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, threads));
+    if (lists->n <= AP_EMBED_FEW_WEIGHTS) {
+#define AP_FEW(A, B) hipLaunchKernelGGL((k_embed_grad_weights_few<A, B>), dim3((unsigned)div_up(lists->n, 4)), dim3(256), 0, st, p, g, ldb, grad_weights)
+        AP_TYPES(dtype, grad_dtype, AP_FEW);
+#undef AP_FEW
+        return AP_OK;
+    }
+    const ApSlabs s = slabs_of((int64_t)slabs * 256, div_up(lists->n, 256));
     AP_REQUIRE(slab_blocks(s) < (1ll << 23), "too many entries");
     const dim3 grid((unsigned)slab_blocks(s)), flat((unsigned)std::min<int64_t>(div_up(lists->n, 256), 8192));
     float *parts = slabs > 1 ? static_cast<float *>(workspace) : grad_weights;
-    int32_t *rows = lists->indptr && row_bytes ? reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + part_bytes) : nullptr;
+    int32_t *rows = lists->indptr ? reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + part_bytes) : nullptr;
     if (rows) AP_TRY(list_rows(p, rows, st));
-#define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(threads), 0, st, p, s, rows, g, ldb, parts)
+#define AP_WEIGHTS(A, B) hipLaunchKernelGGL((k_embed_grad_weights<A, B>), grid, dim3(256), 0, st, p, s, rows, g, ldb, parts)
     AP_TYPES(dtype, grad_dtype, AP_WEIGHTS);
 #undef AP_WEIGHTS
     if (slabs > 1) hipLaunchKernelGGL(k_embed_grad_weights_sum, flat, dim3(256), 0, st, parts, lists->n, slabs, grad_weights);

@@ -142,6 +142,28 @@ def test_gradient_of_the_weights(dtype, grad_dtype, dim, stride):
     near(got, want, size, dim, F32)
 
 
+@pytest.mark.parametrize("dtype,grad_dtype,dim,rows,lists", [(F32, F32, 260, 4_500, True), (BF16, BF16, 264, 9, False), (BF16, F32, 72, 33_001, False), (BF16, BF16, 136, 4_500, True)])
+def test_gradient_of_many_weights(dtype, grad_dtype, dim, rows, lists):
+    rng = np.random.default_rng(dim)
+    indptr, tokens, weights = lists_of(rng, rows, 60, 19 if rows > 9 else 20_000)
+    if not lists:
+        indptr, rows = None, len(tokens)
+    table, grad = matrix(rng, 60, dim, dtype), matrix(rng, rows, dim, grad_dtype)
+    assert len(tokens) > 32_768
+    got = B.embed_grad_weights(grad, table, tokens.to(DEV), None if indptr is None else indptr.to(DEV), scale=3.0)
+    _, _, (want, size) = plain(table, indptr, tokens, weights, 3.0, grad)
+    near(got, want, size, dim, F32)
+
+
+@pytest.mark.parametrize("few", [0, 1])
+def test_lists_with_broken_offsets_have_no_gradient(debug_knobs, few):
+    debug_knobs("embed_few", few)
+    tokens, indptr = torch.arange(5, dtype=torch.int32, device=DEV), torch.tensor([0, 2, 1, 9], device=DEV)
+    table, grad = torch.ones((8, 8), device=DEV), torch.ones((3, 8), device=DEV)
+    assert B.embed_grad(grad, tokens, 8, None, indptr)[:, 0].tolist() == [1.0, 1.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0]
+    assert B.embed_grad_weights(grad, table, tokens, indptr).tolist() == [8.0, 8.0, 0.0, 0.0, 0.0]
+
+
 def test_gradients_are_the_rows_differences():
     """out is linear in the table and in the weights: <G, out(T + D) - out(T)> = <dT, D>, and so for the weights."""
     rng = np.random.default_rng(3)
