@@ -168,17 +168,18 @@ __global__ __launch_bounds__(256) void k_embed_zero(uint4 *__restrict__ p, int64
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = make_uint4(0, 0, 0, 0);
 }
 
-// Zeros to the rows that no entry names: 16 lanes a row.  Bound by its stores: 39 us where 1.2M Zipf(1.1) entries leave three of five of 250,002 rows.
-__global__ __launch_bounds__(256) void k_embed_zero_unnamed(char *__restrict__ out, int64_t row_bytes, int64_t vocab, const uint8_t *__restrict__ named) {
-    const int64_t groups = (int64_t)gridDim.x * 16;
-    for (int64_t r = blockIdx.x * (int64_t)16 + (threadIdx.x >> 4); r < vocab; r += groups * 4) {
+// Zeros to the rows that no entry names, by `blocks` workgroups: 16 lanes a row.
+struct ApUnnamed { char *out; int64_t row_bytes, vocab; const uint8_t *named; int32_t blocks; };
+__device__ __forceinline__ void zero_unnamed(const ApUnnamed &u, int32_t block) {
+    const int64_t groups = (int64_t)u.blocks * 16;
+    for (int64_t r = block * (int64_t)16 + (threadIdx.x >> 4); r < u.vocab; r += groups * 4) {
         bool is[4];
 #pragma unroll
-        for (int k = 0; k < 4; k++) is[k] = r + k * groups < vocab && !named[r + k * groups];
+        for (int k = 0; k < 4; k++) is[k] = r + k * groups < u.vocab && !u.named[r + k * groups];
 #pragma unroll
         for (int k = 0; k < 4; k++)
             if (is[k])
-                for (int64_t c = (threadIdx.x & 15) * 16; c < row_bytes; c += 256) *reinterpret_cast<uint4 *>(out + (r + k * groups) * row_bytes + c) = make_uint4(0, 0, 0, 0);
+                for (int64_t c = (threadIdx.x & 15) * 16; c < u.row_bytes; c += 256) *reinterpret_cast<uint4 *>(u.out + (r + k * groups) * u.row_bytes + c) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -201,6 +202,28 @@ __device__ __forceinline__ int64_t wave_row_of(const int64_t *indptr, int64_t ro
         lo += (k - 1) * step;
         if (step == 1) break;
     }
+    return indptr[lo] <= e && e < indptr[lo + 1] && ap_row_ok(indptr, lo, n) ? lo : -1;
+}
+
+// The lists that a wave's entries lie in, from entry e0 to e1: each half of the wave finds one end, 32 offsets at a time, and every lane its own between them.
+__device__ __forceinline__ void wave_ends_of(const int64_t *indptr, int64_t rows, int64_t e0, int64_t e1, int64_t *first, int64_t *last) {
+    const int lane = threadIdx.x & 63;
+    const int64_t e = lane < 32 ? e0 : e1;
+    int64_t lo = 0, hi = rows;
+    while (__any(hi - lo > 1)) {
+        const int64_t step = (hi - lo + 31) / 32, m = lo + (lane & 31) * step;
+        const uint64_t mask = __ballot(m < hi && (m == lo || indptr[m] <= e));
+        const uint32_t past = ~(uint32_t)(lane < 32 ? mask : mask >> 32);
+        const int k = past ? __builtin_ctz(past) : 32;   // the first k are not past the entry; the first of all never is
+        hi = step == 1 ? lo + k : min(hi, lo + k * step);
+        lo += (k - 1) * step;
+    }
+    *first = __shfl((int)lo, 0, 64);
+    *last = __shfl((int)lo, 32, 64);
+}
+__device__ __forceinline__ int64_t row_between(const int64_t *indptr, int64_t first, int64_t last, int64_t n, int64_t e) {
+    int64_t lo = first, hi = max(first, last) + 1;
+    while (hi - lo > 1) { const int64_t m = (lo + hi) / 2; if (indptr[m] <= e) lo = m; else hi = m; }
     return indptr[lo] <= e && e < indptr[lo + 1] && ap_row_ok(indptr, lo, n) ? lo : -1;
 }
 
@@ -304,12 +327,16 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(ApEmbed p, int32_t owner
 #define AP_SORT_MANY 2048
 #define AP_SORT_ITEMS(n) ((n) > (1 << 18) ? AP_SORT_MANY : AP_SORT_SOME)
 #define AP_SORT_BINS 512
+// Up to as many blocks, each adds up the others' counts by itself, which saves two launches: 15,000 entries of 384 with those of the list of every entry 49 us in
+// all instead of 62.
+#define AP_SORT_TOGETHER 64
 __device__ __forceinline__ uint32_t sort_key(const int32_t *tokens, int64_t vocab, int64_t i) { const int32_t t = tokens[i]; return t >= 0 && t < vocab ? (uint32_t)t : (uint32_t)vocab; }
 
 // Counts of a block's digits.  1.2M entries: 9 us, half of it waiting.  pairs: NULL in the first pass, which takes the tokens
 __global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ tokens, int64_t vocab, const uint2 *__restrict__ pairs, int64_t n, int items, int shift, int bits,
-                                                    uint32_t *__restrict__ hist, int64_t blocks) {
+                                                    uint32_t *__restrict__ hist, int64_t blocks, bool together /* a block's counts */, uint32_t *__restrict__ clear, int64_t words) {
     __shared__ uint32_t s_cnt[AP_SORT_BINS];
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) clear[i] = 0;   // the marks, in the first pass
     for (int b = threadIdx.x; b < 1 << bits; b += 256) s_cnt[b] = 0;
     __syncthreads();
     const int64_t i0 = (int64_t)blockIdx.x * items;
@@ -325,7 +352,7 @@ __global__ __launch_bounds__(256) void k_sort_count(const int32_t *__restrict__ 
             if (k[j] != 0xffffffffu) atomicAdd(&s_cnt[(k[j] >> shift) & ((1 << bits) - 1)], 1u);
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < 1 << bits; b += 256) hist[b * blocks + blockIdx.x] = s_cnt[b];
+    for (int b = threadIdx.x; b < 1 << bits; b += 256) hist[together ? ((int64_t)blockIdx.x << bits) + b : b * blocks + blockIdx.x] = s_cnt[b];
 }
 // A wave makes the counts of a bin into sums over the blocks before, and leaves the bin's total behind them.  Waits for memory: 6 us with 586 blocks.
 __global__ __launch_bounds__(256) void k_sort_scan(uint32_t *__restrict__ hist, int64_t blocks, int bins, uint32_t *__restrict__ totals) {
@@ -365,7 +392,8 @@ static int list_rows(const ApEmbed &p, int32_t *row, hipStream_t st) {
 // 42 us so.
 struct ApSorted { uint2 *of; float *w; };   // of: key and row, after the last pass row and weight
 template <int ITEMS>
-__global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, int shift, int bits, const uint32_t *__restrict__ hist, int64_t blocks, const uint32_t *__restrict__ totals, int last,
+__global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, int shift, int bits, const uint32_t *__restrict__ hist, int64_t blocks,
+                                                      const uint32_t *__restrict__ totals /* NULL: hist has the blocks' counts as they are */, int last,
                                                       const int32_t *__restrict__ rows, uint32_t *__restrict__ keys_out, ApSorted out, uint8_t *__restrict__ named /* or NULL */) {
     __shared__ uint32_t s_at[4][AP_SORT_BINS], s_base[AP_SORT_BINS], s_wave[2][4];
     __shared__ uint2 s_of[ITEMS];
@@ -376,6 +404,12 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, in
     const uint32_t mask = (1u << bits) - 1;
     const int i0 = wave * (ITEMS / 4) + lane;   // a wave's entries lie together
     const bool weighted = p.weights != nullptr;
+    int64_t first_row = 0, last_row = 0;
+    const bool look = !in.of && !rows && p.indptr;   // no list of every entry has been made
+    if (look) {
+        const int64_t e0 = b0 + wave * (ITEMS / 4);
+        wave_ends_of(p.indptr, p.rows, e0, min(e0 + ITEMS / 4, p.n) - 1, &first_row, &last_row);
+    }
     uint2 own[EACH];                            // all asked for at once
     float w[EACH];
 #pragma unroll
@@ -388,7 +422,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, in
             own[k] = in.of[e];
             if (weighted) w[k] = in.w[e];
         } else {
-            own[k] = make_uint2(sort_key(p.tokens, p.vocab, e), rows ? (uint32_t)rows[e] : (uint32_t)e);
+            own[k] = make_uint2(sort_key(p.tokens, p.vocab, e), rows ? (uint32_t)rows[e] : look ? (uint32_t)row_between(p.indptr, first_row, last_row, p.n, e) : (uint32_t)e);
             if (weighted) w[k] = p.weights[e];
         }
     }
@@ -400,10 +434,26 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, in
     __syncthreads();
     {   // where the bins begin, here and among all: two of them a thread
         const uint32_t b = threadIdx.x * 2;
-        uint32_t here_of[2] = {0, 0}, all[2] = {0, 0};
+        uint32_t here_of[2] = {0, 0}, all[2] = {0, 0}, before[2] = {0, 0};
+        if (totals) {
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+                if (b + k <= mask) { all[k] = totals[b + k]; before[k] = hist[(b + k) * blocks + blockIdx.x]; }
+        } else if (b <= mask) {
+            for (int i = 0; i < (int)blocks; i += 16) {
+                uint2 v[16];
+#pragma unroll
+                for (int k = 0; k < 16; k++) v[k] = i + k < (int)blocks ? *reinterpret_cast<const uint2 *>(hist + ((int64_t)(i + k) << bits) + b) : make_uint2(0, 0);
+#pragma unroll
+                for (int k = 0; k < 16; k++) {
+                    all[0] += v[k].x;
+                    all[1] += v[k].y;
+                    if (i + k < (int)blockIdx.x) { before[0] += v[k].x; before[1] += v[k].y; }
+                }
+            }
+        }
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-            if (b + k <= mask) all[k] = totals[b + k];
 #pragma unroll
             for (int w = 0; w < 4; w++) here_of[k] += s_at[w][b + k];
         }
@@ -419,7 +469,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, in
         sum -= all[0] + all[1];
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-            if (b + k <= mask) s_base[b + k] = sum + hist[(b + k) * blocks + blockIdx.x] - here;   // modulo 2^32
+            if (b + k <= mask) s_base[b + k] = sum + before[k] - here;   // modulo 2^32
             uint32_t at = here;
 #pragma unroll
             for (int w = 0; w < 4; w++) { const uint32_t c = s_at[w][b + k]; s_at[w][b + k] = at; at += c; }
@@ -465,8 +515,10 @@ struct ApRuns { const uint32_t *keys; const uint2 *of; float *carry; int32_t run
 // carry[column / 64][which][run][column % 64]: what the joining reads of a token's runs lies together
 __device__ __forceinline__ float *carry_at(const ApRuns &s, int64_t run, int which, int32_t col) { return s.carry + ((col / 64 * 2 + which) * s.runs + run) * 64 + col % 64; }
 template <int GT, int OT>
-__global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, ApSlabs sl) {
+__global__ __launch_bounds__(256) void k_embed_grad_runs(ApEmbed p, ApRuns s, ApSlabs sl, ApUnnamed u) {
     constexpr int N = ApRow16<GT>::N;
+    const int32_t mine_of = (int32_t)blockIdx.x - (int32_t)(gridDim.x - u.blocks);
+    if (mine_of >= 0) { zero_unnamed(u, mine_of); return; }
     int32_t slab;
     int64_t unit;
     if (!slab_block(sl, &slab, &unit)) return;
@@ -758,9 +810,13 @@ extern "C" int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vo
     return AP_OK;
 }
 
-#define AP_RUNS 8192   // 1.2M entries x 1,024: runs of 64, 128 and 256 with their joining take 220, 229 and 228 us
+// How long the runs are: 32 entries while runs times 64 columns are few, or too few loads are on their way; long ones leave fewer sums behind.  From 16, 32 or 64
+// on, 13,400 entries of 384 take 35, 35 and 41 us in all, 32,000 of 768 51, 50 and 55, 250,000 of 128 in bf16 69, 66 and 67; 1.2M of 1,024 with runs of 64, 128
+// and 256 220, 229 and 228 for the runs and their joining.
+#define AP_RUN_LEAST 32
+#define AP_RUNS 65536
 // Whether the rows that entries name are marked, so that zeros go to the others only: not where three quarters are others anyhow.  1.2M entries over 250,002 rows of
-// 2 KB: 39 us of zeros and 4 before the marks instead of 67; 250,000 entries over 100,000: 25 instead of 29.
+// 2 KB: runs and zeros in one launch 234 us, all rows' zeros before the runs 277; 250,000 entries over 100,000: 168 and 186.
 #define AP_EMBED_NAMED(n, vocab) ((vocab) <= 4 * (n))
 struct GradWs {
     int64_t blocks, runs;
@@ -778,8 +834,8 @@ struct GradWs {
         passes = (int32_t)div_up(all, 9);
         bits = (int32_t)div_up(all, passes);
         blocks = div_up(n, AP_SORT_ITEMS(n));
-        run = 64;   // as long as they fill the compute units: every run leaves two rows of sums behind
-        while (run < 256 && n / run > AP_RUNS) run *= 2;
+        run = AP_RUN_LEAST;
+        while (run < 256 && n / run * div_up(dim, 64) > AP_RUNS) run *= 2;
         runs = div_up(n, run);
         for (int i = 0; i < 2; i++) { sorted[i].of = (uint2 *)take(2 * n); sorted[i].w = (float *)take(n); }
         keys = (uint32_t *)take(n);
@@ -828,33 +884,30 @@ extern "C" int ap_embed_grad(const void *grad_out, int64_t ld, int32_t dtype, in
 #undef AP_FEW
         return AP_OK;
     }
-    if (marked) AP_TRY(ap_fill_u32(ws.named, (size_t)div_up(vocab, 4), 0, st));
-    if (lists->indptr) AP_TRY(list_rows(p, ws.rows, st));
     const int items = AP_SORT_ITEMS(lists->n);
+    const bool listed = lists->indptr && items == AP_SORT_MANY, together = ws.blocks <= AP_SORT_TOGETHER;
+    if (listed) AP_TRY(list_rows(p, ws.rows, st));
     for (int i = 0; i < ws.passes; i++) {
         const ApSorted in = i ? ws.sorted[(i - 1) & 1] : ApSorted{nullptr, nullptr};
-        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, in.of, lists->n, items, i * ws.bits, ws.bits, ws.hist, ws.blocks);
-        hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)div_up(1 << ws.bits, 4)), dim3(256), 0, st, ws.hist, ws.blocks, 1 << ws.bits, ws.totals);
+        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)ws.blocks), dim3(256), 0, st, lists->tokens, vocab, in.of, lists->n, items, i * ws.bits, ws.bits, ws.hist, ws.blocks, together,
+                           reinterpret_cast<uint32_t *>(ws.named), marked && i == 0 ? div_up(vocab, 4) : 0);
+        if (!together) hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)div_up(1 << ws.bits, 4)), dim3(256), 0, st, ws.hist, ws.blocks, 1 << ws.bits, ws.totals);
 #define AP_SCATTER(ITEMS)                                                                                                                                                    \
-    hipLaunchKernelGGL(k_sort_scatter<ITEMS>, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, in, i * ws.bits, ws.bits, ws.hist, ws.blocks, ws.totals, i + 1 == ws.passes, \
-                       lists->indptr ? ws.rows : nullptr, ws.keys, ws.sorted[i & 1], marked ? ws.named : nullptr)
+    hipLaunchKernelGGL(k_sort_scatter<ITEMS>, dim3((unsigned)ws.blocks), dim3(256), 0, st, p, in, i * ws.bits, ws.bits, ws.hist, ws.blocks, together ? nullptr : ws.totals, i + 1 == ws.passes, \
+                       listed ? ws.rows : nullptr, ws.keys, ws.sorted[i & 1], marked ? ws.named : nullptr)
         if (items == AP_SORT_MANY) AP_SCATTER(AP_SORT_MANY); else AP_SCATTER(AP_SORT_SOME);
 #undef AP_SCATTER
-        AP_CHECK_HIP(hipGetLastError());
-    }
-    if (marked) {
-        const int64_t row_bytes = (int64_t)dim * (table_dtype == AP_BF16 ? 2 : 4);
-        hipLaunchKernelGGL(k_embed_zero_unnamed, dim3((unsigned)std::min<int64_t>(div_up(vocab, 64), 4096)), dim3(256), 0, st, static_cast<char *>(grad_table), row_bytes, vocab, ws.named);
         AP_CHECK_HIP(hipGetLastError());
     }
     const ApRuns s{ws.keys, ws.sorted[(ws.passes - 1) & 1].of, ws.carry, ws.run, ws.runs};
     const ApSlabs sl = slabs_of((int64_t)dim * (dtype == AP_BF16 ? 2 : 4), div_up(ws.runs, 16));
     AP_REQUIRE(slab_blocks(sl) < (1ll << 23), "too many entries");
-    const dim3 grid((unsigned)slab_blocks(sl));
+    const ApUnnamed u{static_cast<char *>(grad_table), (int64_t)dim * (table_dtype == AP_BF16 ? 2 : 4), vocab, ws.named, marked ? (int32_t)std::min<int64_t>(div_up(vocab, 64), 4096) : 0};
+    const dim3 grid((unsigned)(slab_blocks(sl) + u.blocks));
     const int64_t heads = div_up(ws.runs, 16), most = (1ll << 22) / heads;   // below 2^31 threads
     const int32_t wide = (int32_t)std::max<int64_t>(1, std::min(div_up(dim, 256), most));
     const dim3 joins((unsigned)heads, (unsigned)(wide + std::max<int64_t>(1, std::min(div_up(dim, 64), most))));
-#define AP_RUNS(A, B) hipLaunchKernelGGL((k_embed_grad_runs<A, B>), grid, dim3(256), 0, st, p, s, sl)
+#define AP_RUNS(A, B) hipLaunchKernelGGL((k_embed_grad_runs<A, B>), grid, dim3(256), 0, st, p, s, sl, u)
     AP_TYPES(dtype, table_dtype, AP_RUNS);
 #undef AP_RUNS
     if (table_dtype == AP_F32) hipLaunchKernelGGL((k_embed_grad_join<AP_F32>), joins, dim3(256), 0, st, p, s, wide);

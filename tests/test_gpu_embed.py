@@ -120,6 +120,7 @@ def test_gradient_of_many_tokens(vocab, n, dim):
 @pytest.mark.parametrize("counts,dim,table_dtype", [
     ([64, 128, 64 * 16, 64 * 17, 64 * 18, 63, 1, 65], 72, F32),           # tokens that end with a run, of up to and over 16 runs
     ([1, 64 * 17 - 1, 64 * 17, 64 * 17 + 1, 2, 64 * 40 + 5], 520, BF16),
+    ([32, 32 * 16, 31, 32 * 17, 1, 32 * 18 - 1, 33, 32 * 50], 24, F32), ([5] * 800 + [32 * 16 + 1] * 2, 1000, BF16),
     ([30_000] * 10 + [3] * 100, 8, F32)])                                  # longer blocks of the sort
 def test_gradient_of_tokens_over_many_runs(counts, dim, table_dtype):
     rng = np.random.default_rng(len(counts))
