@@ -164,11 +164,10 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE, bo
     // product takes `parts` = 3 pairs: second times first, first times second, first times first (the smallest first; the product
     // of the second parts is below the last bit of the sum).  2: only one operand has a second part, and the other's `.._part` is 0.
     static __device__ __forceinline__ void product(const ApOperand &A, const ApOperand &B, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB]) {
-        run<false>([&](int32_t, ApOperand &a, ApOperand &b) { a = A; b = B; }, 1, K, parts, a_part, b_part, lds, acc, [](int32_t) { return false; });
+        run<false>([&](int32_t, ApOperand &a, ApOperand &b) { a = A; b = B; }, 1, K, parts, a_part, b_part, lds, acc, [](int32_t) {});
     }
     // The products of tiles 0 .. count - 1, one after the other without a pause: while a tile is finished the next one's first chunks come, so both
-    // stages stay in use.  tile_of(i, a, b) sets the operands of a tile, up to three tiles ahead, and may bring more into LDS for it; done(i) takes acc and says whether it has issued 56 stores or more, behind
-    // which the loads of the next chunk need not be waited for (memory operations of a wave end in their order).
+    // stages stay in use.  tile_of(i, a, b) sets the operands of a tile, up to three tiles ahead, and may bring more into LDS for it; done(i) takes acc.
     template <class T, class D>
     static __device__ __forceinline__ void products(T tile_of, int32_t count, int32_t K, int parts, int64_t a_part, int64_t b_part, char *lds, Acc (&acc)[FA][FB], D done) {
         run<true>(tile_of, count, K, parts, a_part, b_part, lds, acc, done);
@@ -248,7 +247,7 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE, bo
 #pragma unroll
             for (int i = 0; i < NM; i++) total[i / FB][i % FB] = Acc{0, 0, 0, 0};
         static_assert(!MANY || OP::BYTES != 4, "f32 sums are of one tile");
-        int32_t c = 0, st = 0, at = 0, behind_stores = 0;
+        int32_t c = 0, st = 0, at = 0;
         while (MANY ? at < count : c < chunks) {
 #pragma unroll
             for (int i = 0; i < NM; i++) {
@@ -259,8 +258,7 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE, bo
 #pragma unroll
             for (int i = 0; i < MEET; i++) mul(1, i);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (MANY) asm volatile("s_waitcnt vmcnt(56)\n\ts_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(0)\n1:" ::"s"(behind_stores) : "memory", "scc");
-            else ap_g_wait_loads<0>();
+            ap_g_wait_loads<0>();   // also for a finished tile's stores, which have had a step and more to leave
             ap_g_barrier();
             // past the last chunk nothing is left: the loads bring zeros that nobody reads
             const char *a = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_a)), *b = reinterpret_cast<const char *>(ap_uniform_u64((uint64_t)next_b));
@@ -286,9 +284,8 @@ template <class OP, int TM, int TN, int WM, int WN, bool A_LINE, bool B_LINE, bo
             st ^= 1;
             c++;
             if constexpr (MANY) {
-                behind_stores = 0;
                 if (c == chunks) {
-                    behind_stores = ap_uniform_i32(done(at));
+                    done(at);
                     clear();
                     c = 0;
                     at++;

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_scores8_many(ApScores8 p) {
                     lds_barrier();
                 }
             }
-            return false;
+            return;
         }
         auto put = [&](auto all) {
 #pragma unroll
@@ -291,7 +291,6 @@ __global__ __launch_bounds__(WM *WN * 64) void k_scores8_many(ApScores8 p) {
             }
         };
         if (whole) put(std::true_type{}); else put(std::false_type{});
-        return false;
     };
     G::products(tile_of, (int32_t)((nts * mts - blockIdx.x + gridDim.x - 1) / gridDim.x), p.pad, 1, 0, 0, lds, acc, done);
 }

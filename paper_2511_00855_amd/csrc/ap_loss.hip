@@ -354,7 +354,6 @@ __global__ __launch_bounds__(512) void k_loss_coefs(ApLoss p) {
                 }
             }
         }
-        return false;
     };
     G::products(tile_of, (int32_t)((mts * nts - blockIdx.x + gridDim.x - 1) / gridDim.x), p.dim, PARTS ? 3 : 1, p.x_part, p.d_part, lds, acc, done);
 }
