@@ -510,7 +510,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(ApEmbed p, ApSorted in, in
 
 // 16 lanes take a run of `run` sorted entries and a slab.  Tokens whose entries all lie in the run are written; the sum of a token that began
 // in an earlier run goes to carry[run][0], that of one that goes on in the next to carry[run][1].  Bound by what the L2s gather: 1.2M entries of bf16
-// rows of 1,024 (2.46 GB) take 210 us, 11.7 TB/s; 20,000 rows of a slab are 5 MB, a little more than an L2, and six lines of ten are hits.
+// rows of 1,024 (2.46 GB) take 210 us, 11.7 TB/s, and 234 with the other rows' zeros (318 MB); 20,000 rows of a slab are 5 MB, a little more than an L2, and six lines of ten are hits.
 struct ApRuns { const uint32_t *keys; const uint2 *of; float *carry; int32_t run; int64_t runs; };   // of: an entry's row and weight
 // carry[column / 64][which][run][column % 64]: what the joining reads of a token's runs lies together
 __device__ __forceinline__ float *carry_at(const ApRuns &s, int64_t run, int which, int32_t col) { return s.carry + ((col / 64 * 2 + which) * s.runs + run) * 64 + col % 64; }

@@ -177,7 +177,7 @@ template <bool F16> __device__ __forceinline__ uint2 ap_coef_part(float (&v)[4])
 }
 
 // GRAD: the tile's coefficients (tiles of 128 and 64; k_loss_coefs has the largest).  Otherwise its maximum and sum a query.  Bound by the matrix
-// instruction and the card's power: 4,096 queries over 250,002 bf16 rows of 1,024 take 1,860 us (1,130 TFLOP/s), 2,048 over 100,000 f32 rows of 768 in
+// instruction (busy 56 % of the cycles; two thirds within a product, the rest is the exponentials): 4,096 queries over 250,002 bf16 rows of 1,024 take 1,860 us (1,130 TFLOP/s), 2,048 over 100,000 f32 rows of 768 in
 // parts 870 us (1,085 of f16 products); 100 over 2,000 f32 rows of 128 take 7 us, and there a launch is most of it.
 template <class OP, int TM, int TN, int WM, int WN, bool PARTS, bool GRAD>
 __global__ __launch_bounds__(WM *WN * 64) void k_loss_tiles(ApLoss p) {
@@ -535,7 +535,7 @@ struct ApLossGrad {
 };
 
 // A piece's share of both gradients out of its coefficients: the first workgroups take the queries' (runs of the documents), the others the documents'.
-// Bound by the matrix instruction and the card's power: 4,096 queries x 16,128 documents x 1,024 in bf16 take 211 us (1,280 TFLOP/s), 2,048 x 32,768 x 768 in
+// Bound by the matrix instruction (busy 63 % of the cycles): 4,096 queries x 16,128 documents x 1,024 in bf16 take 211 us (1,280 TFLOP/s), 2,048 x 32,768 x 768 in
 // parts 545 us (1,135 of f16 products).
 template <class OP, int TM, int TN, int WM, int WN, bool PARTS>
 __global__ __launch_bounds__(WM *WN * 64) void k_loss_grads(ApLossGrad p) {
