@@ -535,12 +535,14 @@ class Index:
 # -- learning the dense rows, and holding them in 8 bits -----------------------
 def _rows(t: torch.Tensor, what: str):
     """(address, elements from row to row, dtype code) of a matrix of f32 or bf16 rows; int16 is bf16 as DeviceVecs keeps it."""
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()   # each is a call: read once
+    if len(shape) != 2 or not t.is_cuda or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{what} must be a matrix on the GPU whose rows are contiguous")
-    code = AP_F32 if t.dtype is torch.float32 else AP_BF16 if t.dtype in (torch.bfloat16, torch.int16) else None
+    dtype = t.dtype
+    code = AP_F32 if dtype is torch.float32 else AP_BF16 if dtype is torch.bfloat16 or dtype is torch.int16 else None
     if code is None:
-        raise ValueError(f"{what} must be f32 or bf16, not {t.dtype}")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8, code   # a single row has no next one
+        raise ValueError(f"{what} must be f32 or bf16, not {dtype}")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else -(-shape[1] // 8) * 8, code   # a single row has no next one
 
 
 def _vec(t: torch.Tensor, dtype, count: int, device, what: str):
@@ -559,7 +561,7 @@ def _bytes_of(fn: str, args) -> int:
 
 def _call(fn: str, device, *args, bytes_args=None):
     """Calls ap_<fn> on the device's current stream, with the workspace that ap_<fn>_bytes(*bytes_args) asks for."""
-    if torch.cuda.current_device() != device.index:
+    if torch._C._cuda_getDevice() != device.index:
         with torch.cuda.device(device):
             return _call(fn, device, *args, bytes_args=bytes_args)
     L = lib()
@@ -584,9 +586,13 @@ _DTYPE = {torch.float32: AP_F32, torch.bfloat16: AP_BF16}
 
 def _lists(tokens, weights, indptr, device) -> _Lists:
     n = tokens.numel()
-    rows = n if indptr is None else indptr.numel() - 1
-    return _Lists(rows, n, None if indptr is None else _vec(indptr, torch.int64, rows + 1, device, "indptr"), _vec(tokens, torch.int32, n, device, "tokens"),
-                  None if weights is None else _vec(weights, torch.float32, n, device, "weights"))
+    t = _vec(tokens, torch.int32, n, device, "tokens")
+    if indptr is None:
+        rows, i = n, None
+    else:
+        rows = indptr.numel() - 1
+        i = _vec(indptr, torch.int64, rows + 1, device, "indptr")
+    return _Lists(rows, n, i, t, None if weights is None else _vec(weights, torch.float32, n, device, "weights"))
 
 
 def embed(table: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Tensor] = None, indptr: Optional[torch.Tensor] = None, scale: float = 1.0,
@@ -594,9 +600,10 @@ def embed(table: torch.Tensor, tokens: torch.Tensor, weights: Optional[torch.Ten
     """Dense rows out of token lists (see ap_embed): scale times the weighted sum of the table's rows that a list names, a row a list; without
     indptr a row a token.  out_dtype: float32 or bfloat16, the table's own if None."""
     p, ld, code = _rows(table, "table")
-    l = _lists(tokens, weights, indptr, table.device)
-    out = torch.empty((l.rows, table.shape[1]), dtype=out_dtype or table.dtype, device=table.device)
-    _call("ap_embed", table.device, p, ld, code, table.shape[0], table.shape[1], C.byref(l), scale, out.data_ptr(), code if out_dtype is None else _DTYPE[out_dtype])
+    (vocab, dim), device = table.shape, table.device
+    l = _lists(tokens, weights, indptr, device)
+    out = torch.empty(l.rows, dim, dtype=out_dtype or table.dtype, device=device)   # sizes one by one are read faster than a tuple of them
+    _call("ap_embed", device, p, ld, code, vocab, dim, C.byref(l), scale, out.data_ptr(), code if out_dtype is None else _DTYPE[out_dtype])
     return out
 
 
@@ -608,7 +615,7 @@ def embed_grad(grad_out: torch.Tensor, tokens: torch.Tensor, vocab: int, weights
     if l.rows != grad_out.shape[0]:
         raise ValueError(f"grad_out has {grad_out.shape[0]} rows for {l.rows} lists")
     dim = grad_out.shape[1]
-    out = torch.empty((vocab, dim), dtype=dtype or grad_out.dtype, device=grad_out.device)
+    out = torch.empty(vocab, dim, dtype=dtype or grad_out.dtype, device=grad_out.device)
     _call("ap_embed_grad", grad_out.device, p, ld, code, dim, C.byref(l), vocab, scale, out.data_ptr(), code if dtype is None else _DTYPE[dtype], bytes_args=(l.n, vocab, dim))
     return out
 
@@ -636,7 +643,7 @@ def quantize_rows(x: torch.Tensor):
     """Rows in 8 bits with a scale each (see ap_quantize_rows): (int8, as many columns as x rounded up to a multiple of 16; f32)."""
     p, ld, code = _rows(x, "x")
     rows, dim = x.shape
-    q = torch.empty((rows, -(-dim // 16) * 16), dtype=torch.int8, device=x.device)
+    q = torch.empty(rows, -(-dim // 16) * 16, dtype=torch.int8, device=x.device)
     scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     _call("ap_quantize_rows", x.device, p, ld, rows, dim, code, q.data_ptr(), q.shape[1], scale.data_ptr())
     return q, scale
@@ -657,7 +664,7 @@ def scores_int8(x: torch.Tensor, q: torch.Tensor, q_scale: torch.Tensor, x_scale
         raise ValueError("x and q differ in device or number of columns")
     sq = _vec(q_scale, torch.float32, n, x.device, "q_scale")
     sx = None if x_scale is None else _vec(x_scale, torch.float32, rows, x.device, "x_scale")
-    out = torch.empty((rows, n), dtype=torch.float32, device=x.device)
+    out = torch.empty(rows, n, dtype=torch.float32, device=x.device)
     _call("ap_scores_int8", x.device, px, ldx, sx, rows, dim, code, pq, ldq, sq, n, out.data_ptr(), n, bytes_args=(rows, dim, code))
     return out
 
@@ -672,7 +679,7 @@ def softmax_loss(x: torch.Tensor, docs: torch.Tensor, labels: torch.Tensor, scal
         raise ValueError("x and docs differ in type")
     (rows, dim), n = x.shape, docs.shape[0]
     labels_p = _vec(labels, torch.int32, rows, x.device, "labels")
-    loss, lse = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    loss, lse = torch.empty(2, rows, dtype=torch.float32, device=x.device)
     _call("ap_softmax_loss", x.device, px, ldx, rows, pd, ldd, n, dim, code, scale, labels_p, loss.data_ptr(), lse.data_ptr(), bytes_args=(rows, n, dim, code))
     return loss, lse
 

@@ -69,7 +69,7 @@ def test_embed():
     refused(L.ap_embed_grad(A, 16, 0, 16, C.byref(B._Lists(100_000, 100_000, None, A, None)), 9, 1.0, A, 0, A, 64, None), "workspace")
     refused(L.ap_embed_grad_weights(A, 16, 0, A, 16, 0, 9, 16, C.byref(lists), 1.0, None, A, 64, None), "NULL")
     refused(L.ap_embed_grad_weights(A, 12, 0, A, 16, 0, 9, 16, C.byref(lists), 1.0, A, A, 64, None), "row to row")
-    refused(L.ap_embed_grad_weights(A, 256, 0, A, 256, 0, 9, 256, C.byref(lists), 1.0, A, A, 16, None), "workspace")
+    refused(L.ap_embed_grad_weights(A, 256, 0, A, 256, 0, 9, 256, C.byref(B._Lists(100_000, 100_000, None, A, None)), 1.0, A, A, 16, None), "workspace")
 
 
 def test_eight_bits():
