@@ -644,7 +644,7 @@ __global__ __launch_bounds__(256) void k_loss_gx(const float *__restrict__ gx, i
 // loads and stores are whole lines.  16 documents at a time: their rows times the coefficients go to sums of the queries' gradient that stay
 // in registers, the queries (in registers too) times the coefficients are the documents' gradient.
 // Bound by memory up to 16 queries, every byte once in and once out: 120,011 bf16 rows of 1,024 121 us for one (4.1 TB/s), 100,000 f32 rows of 768 131 us for
-// 16 (4.7 TB/s); by the f32 instruction above: 172 us for 32 bf16 queries, 250 for 64 of f32.
+// 16 (4.7 TB/s); by the f32 instruction above: 172 us for 32 bf16 queries.
 struct ApLossFew {
     const char *docs, *x;          // x: without queries of weight 0
     int64_t ldd, ldx;
@@ -817,25 +817,27 @@ static int check_sizes(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
 }
 
 // Up to how many queries passes over the documents pay.  bf16, the loss of 64: 51 us by passes and 57 by tiles over 120,011 rows of 1,024, 136 and 207 over
-// 500,000 of 768; a step: 32 queries over 120,011 of 1,024, 259 and 421, 40 queries 364 and 296, and over 30,522 of 768, 82 and 98, 98 and 87.  f32: a step of
-// 64 over 100,000 rows of 768 566 and 629; over 20,000 of 384, 74 and 78 for 48, 91 and 80 for 64.  f32 takes the same way for the loss and its gradient (form_of).
-#define AP_LOSS_FEW 64
+// 500,000 of 768; a step: 32 queries over 120,011 of 1,024, 261 and 269, 40 queries 366 and 275.  f32, a step over 100,000 rows of 768: 395 and 430 for 48, 557
+// and 433 for 64; over 20,000 of 384, 76 and 79, 91 and 80.  f32 takes the same way for the loss and its gradient (form_of).
+#define AP_LOSS_FEW_F32 48
+#define AP_LOSS_FEW_BF16 64
 #define AP_LOSS_FEW_GRAD_BF16 32
 static int32_t few_group(int64_t row_bytes) { return (int32_t)std::min<int64_t>(64, AP_STREAM_LDS / ((row_bytes + 63) / 64 * 64) / 16 * 16); }   // queries a pass
 static bool loss_few(int64_t rows, int32_t dim, int32_t dtype, bool grad) {
-    const int64_t most = g_ap_debug.loss_few ? std::min<int64_t>(g_ap_debug.loss_few - 1, 64) : dtype == AP_BF16 && grad ? AP_LOSS_FEW_GRAD_BF16 : AP_LOSS_FEW;
+    const int64_t most = g_ap_debug.loss_few ? std::min<int64_t>(g_ap_debug.loss_few - 1, 64) : dtype != AP_BF16 ? AP_LOSS_FEW_F32 : grad ? AP_LOSS_FEW_GRAD_BF16 : AP_LOSS_FEW_BF16;
     return rows <= most && few_group((int64_t)dim * (dtype == AP_BF16 ? 2 : 4)) > 0;
 }
 // How rows are multiplied: bf16 as they are; f32 as they are by the f32 instruction, or as two f16 parts each.  Parts cost two passes over the documents
-// and two launches more, and save most of a product's time.  A step over 100,000 rows of 768 takes 838 us in f32 and 829 in parts for 128 queries, 1,441
-// and 949 for 200; over 20,000 of 384, 119 and 130, and 233 and 152; 100 queries over 2,000 of 128, 41 and 75.  The loss and its gradient go by the
-// same rule: a logit that is off is then off in both.
+// and two launches more, and save most of a product's time.  A step, f32 and parts: over 100,000 rows of 768, 691 and 796 us for 128 queries, 984 and 854 for
+// 140; over 20,000 of 384 131 and 150 for 192, 171 and 151 for 200; over 5,000 of 768 89 and 100 for 192, 116 and 105 for 256; over 5,000 of 260 72 and 73 for
+// 320.  The f32 form's tiles are 64 queries wide, and so are the steps of the rule.  The loss and its gradient go by the same one: a logit that is off is then
+// off in both.
 enum LossForm { LOSS_BF16, LOSS_F32, LOSS_PARTS };
 static LossForm form_of(int64_t rows, int64_t n, int32_t dim, int32_t dtype) {
     if (dtype == AP_BF16) return LOSS_BF16;
     const double work = (double)n * dim;
     if (g_ap_debug.loss_form) return g_ap_debug.loss_form == 1 ? LOSS_F32 : LOSS_PARTS;
-    return loss_few(rows, dim, dtype, false) || rows <= 128 + 3.75e8 / work ? LOSS_F32 : LOSS_PARTS;
+    return loss_few(rows, dim, dtype, false) || up_to(rows, 64) <= 128 + 5e8 / work ? LOSS_F32 : LOSS_PARTS;
 }
 
 struct LossParts {   // f32 rows as two f16 parts
@@ -862,9 +864,11 @@ struct LossParts {   // f32 rows as two f16 parts
     }
 };
 
-// The tile that fills the compute units: the largest of 256, 128, 64 whose tiles are at least 3/4 of them.
+// The tile that fills the compute units: the largest of 256, 128, 64 whose tiles are at least 3/4 of them; always 64 for the f32 instruction, which is so slow
+// that small tiles cost it nothing and share the work out more evenly (a step of 80 queries over 37,740 rows of 500: 256 us with tiles of 128, 190 with 64; 100
+// over 100,000 of 768 825 and 688; only a loss over 64,000 of 1,024 takes 139 us instead of 134).
 static int pick_tile(int64_t m, int64_t n, LossForm form) {
-    for (int t = form == LOSS_F32 ? 128 : 256; t > 64; t /= 2)
+    for (int t = form == LOSS_F32 ? 64 : 256; t > 64; t /= 2)
         if (div_up(m, t) * div_up(n, t) >= 192) return t;
     return 64;
 }
@@ -872,23 +876,22 @@ static int pick_tile(int64_t m, int64_t n, LossForm form) {
 template <class OP, bool PARTS, bool GRAD>
 static int launch_tiles(ApLoss &p, int tile, hipStream_t st) {
     const int64_t mt = div_up(p.count, tile), nt = div_up(p.rows, tile);
-    AP_REQUIRE(mt * nt < (1ll << 31) / 512, "rows x n is too large");
+    AP_REQUIRE(mt * nt < (1ll << 31) / (tile == 256 ? 512 : 256), "rows x n is too large");
     const dim3 grid((unsigned)(mt * nt));
     p.group = (int32_t)std::min<int64_t>(nt, 8);
-    if (tile == 256) {
-        if constexpr (OP::BYTES == 2) {
-            if constexpr (GRAD) hipLaunchKernelGGL((k_loss_coefs<OP, PARTS>), dim3(std::min<unsigned>(grid.x, AP_CUS)), dim3(512), 0, st, p);
-            else hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
-        }
-    } else if (tile == 128) hipLaunchKernelGGL((k_loss_tiles<OP, 128, 128, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((k_loss_tiles<OP, 64, 64, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
+    if (tile == 64) hipLaunchKernelGGL((k_loss_tiles<OP, 64, 64, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
+    else if constexpr (OP::BYTES == 2) {
+        if (tile == 128) hipLaunchKernelGGL((k_loss_tiles<OP, 128, 128, 2, 2, PARTS, GRAD>), grid, dim3(256), 0, st, p);
+        else if constexpr (GRAD) hipLaunchKernelGGL((k_loss_coefs<OP, PARTS>), dim3(std::min<unsigned>(grid.x, AP_CUS)), dim3(512), 0, st, p);
+        else hipLaunchKernelGGL((k_loss_tiles<OP, 256, 256, 2, 4, PARTS, GRAD>), grid, dim3(512), 0, st, p);
+    }
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }
 
 template <int DT, bool GRAD> static int launch_few(const ApLoss &all, hipStream_t st) {
     const int64_t row_bytes = (int64_t)all.dim * (DT == AP_F32 ? 4 : 2), blocks = ap_stream_blocks(all.count);
-    // as many passes as LDS makes it, of queries shared out evenly: 64 over 100,000 f32 rows of 768 take two of 32, 162 us, 48 and 16 165
+    // as many passes as LDS makes it, of queries shared out evenly
     const int32_t passes = (int32_t)div_up(all.rows, few_group(row_bytes)), group = (int32_t)div_up(div_up(all.rows, passes), 16) * 16;
     for (int32_t q0 = 0; q0 < all.rows; q0 += group) {
         ApLoss p = all;
@@ -1059,7 +1062,6 @@ struct GradPlan {
         tile_c = pick_tile(piece, r, form);
         tile = pick_tile(piece, dim, form);
         if (tile > 128 && r <= 128) tile = 128;
-        if (tile > 64 && r <= 64 && form == LOSS_F32) tile = 64;   // 64 queries over 100,000 f32 rows of 768: 629 us, 741 with 128; 64 over 120,011 bf16 rows of 1,024: 465, 325 with 128
         runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts, tile, form);
         run_docs = (int32_t)up_to(div_up(piece, runs), 64);
         runs = (int32_t)div_up(piece, run_docs);
@@ -1095,10 +1097,11 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, ApLossGrad g, int64_t n, 
         // a short last piece leaves the runs past its end alone
         g.runs = (uint32_t)(!g.gx ? 0 : g.start ? plan.runs : div_up(g.count, plan.run_docs));
         const dim3 grid((unsigned)(g.runs * div_up(g.rows, tile) * nt + (g.grad_docs ? div_up(g.count, tile) * nt : 0)));
-        if (tile == 256) {
-            if constexpr (OP::BYTES == 2) hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
-        } else if (tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
-        else hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        if (tile == 64) hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+        else if constexpr (OP::BYTES == 2) {
+            if (tile == 128) hipLaunchKernelGGL((k_loss_grads<OP, 128, 128, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
+            else hipLaunchKernelGGL((k_loss_grads<OP, 256, 256, 2, 4, PARTS>), grid, dim3(512), 0, st, g);
+        }
         AP_CHECK_HIP(hipGetLastError());
     }
     return AP_OK;
