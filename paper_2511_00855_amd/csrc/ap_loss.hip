@@ -864,13 +864,42 @@ struct LossParts {   // f32 rows as two f16 parts
     }
 };
 
-// The tile that fills the compute units: the largest of 256, 128, 64 whose tiles are at least 3/4 of them; always 64 for the f32 instruction, which is so slow
-// that small tiles cost it nothing and share the work out more evenly (a step of 80 queries over 37,740 rows of 500: 256 us with tiles of 128, 190 with 64; 100
-// over 100,000 of 768 825 and 688; only a loss over 64,000 of 1,024 takes 139 us instead of 134).
+// What the tiles of m x n take, in rounds of the largest: one of 256 on every compute unit.  Two of 128 share one and take 0.74 of that time, four of 64 0.47; a round
+// that is not full takes half of one and its share (dispatch is even, but the last tiles run alone).
+static double tiles_cost(int tile, int64_t m, int64_t n) {
+    const int64_t tiles = div_up(m, tile) * div_up(n, tile), round = tile == 256 ? 256 : tile == 128 ? 512 : 1024, left = tiles % round;
+    if (tile == 256) return (double)div_up(tiles, round);
+    return (tile == 128 ? 0.74 : 0.47) * ((double)(tiles / round) + (left ? 0.5 + 0.5 * (double)left / (double)round : 0.));
+}
+// The tile that takes the least; always 64 for the f32 instruction, which is so slow that small tiles cost it nothing and share the work out more evenly (a step of
+// 80 queries over 37,740 rows of 500: 256 us with tiles of 128, 190 with 64; 100 over 100,000 of 768 825 and 688; only a loss over 64,000 of 1,024
+// takes 139 us instead of 134).  bf16, kernel times with 256, 128 and 64: 515 queries over 24,000 rows of 1,024 53, 46 and 54 us; 1,500 over 9,000 33, 46 and 52;
+// 500 over 5,000 of 768 24, 17 and 11.
 static int pick_tile(int64_t m, int64_t n, LossForm form) {
-    for (int t = form == LOSS_F32 ? 64 : 256; t > 64; t /= 2)
-        if (div_up(m, t) * div_up(n, t) >= 192) return t;
-    return 64;
+    int best = 64;
+    if (form != LOSS_F32)
+        for (int t = 128; t <= 256; t *= 2)
+            if (tiles_cost(t, m, n) <= tiles_cost(best, m, n)) best = t;
+    return best;
+}
+// The same for both gradients of a piece with the queries' in `runs` runs, in the lengths of k that a compute unit goes through.
+static double grads_cost(int tile, int64_t runs, int64_t r, int64_t dim, int64_t piece, int64_t parts, bool want_x) {
+    const int64_t over = tile == 256 ? 512 : 256, at_once = tile == 256 ? 256 : 512, cols = div_up(dim, tile);
+    const double a = want_x ? (double)(div_up(piece, runs) * parts + over) : 0., b = (double)(r * parts + over);
+    const double work = ((double)(div_up(r, tile) * cols * runs) * a + (double)(div_up(piece, tile) * cols) * b) / (double)at_once;
+    return std::max(std::max(a, b), work + 0.5 * std::min(a, b)) * (tile == 256 ? 1. : tile == 128 ? 0.85 : 0.32);
+}
+// 3,000 queries over 3,000 rows of 768 with 256, 128 and 64: 63, 47 and 61 us; 515 over 24,000 of 1,024 68, 84 and 110; 300 over 40,000 of 384 48, 39 and 51.
+static int pick_grad_tile(int64_t r, int64_t dim, int64_t piece, int64_t parts, bool want_x, LossForm form, int64_t runs = 0 /* 0: as many as are best */) {
+    if (form == LOSS_F32) return 64;
+    int best = 64;
+    double least = 1e30;
+    for (int t = r <= 128 ? 128 : 256; t >= 64; t /= 2)
+        for (int64_t s = runs ? runs : 1; s <= (runs ? runs : 32) && (s == 1 || runs || piece / s >= 256); s *= 2) {
+            const double cost = grads_cost(t, s, r, dim, piece, parts, want_x);
+            if (cost < least) { least = cost; best = t; }
+        }
+    return best;
 }
 
 template <class OP, bool PARTS, bool GRAD>
@@ -1008,7 +1037,7 @@ static int32_t pick_runs(int64_t tiles, int64_t piece, int64_t more, int64_t k, 
 struct GradPlan {
     LossForm form;
     int64_t piece, ldc, c_part;
-    int tile_c, tile;
+    int tile;
     bool few, two;
     int32_t runs, run_docs;
     float *most, *coef, *gx;
@@ -1016,11 +1045,10 @@ struct GradPlan {
     LossParts parts;
     // What a piece of p documents takes, in the units of pick_runs.
     static double piece_cost(int64_t p, int64_t r, int64_t dim, int64_t parts, bool want_x, LossForm form) {
-        const int64_t tc = pick_tile(p, r, form), t = pick_tile(p, dim, form), more = div_up(p, t) * div_up(dim, t);
-        double cost = (double)(div_up(div_up(p, tc) * div_up(r, tc), 256) * (dim * parts + 512)) * tc * tc / 65536;
+        const int64_t t = pick_grad_tile(r, dim, p, parts, want_x, form), more = div_up(p, t) * div_up(dim, t);
         int64_t least = div_up(more, 256) * (r * parts + 512);
         if (want_x) pick_runs(div_up(r, t) * div_up(dim, t), p, more, r, parts, (int)t, form, &least);
-        return cost + (double)least * t * t / 65536 + 2 * 2048;   // two launches
+        return tiles_cost(pick_tile(p, r, form), p, r) * (double)(dim * parts + 512) + (double)least * (t == 256 ? 1. : t == 128 ? 0.85 : 0.32) + 2 * 2048;   // two launches
     }
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype, bool want_x) {
         LossWs ws{base};
@@ -1046,9 +1074,9 @@ struct GradPlan {
         else if (piece < n) {   // several pieces: the length of which all of them take the least time
             double least = 1e30;
             int64_t best = piece;
-            const int tile_of_all = pick_tile(piece, dim, form);   // the largest tiles take a length of which they fill the compute units
+            const int tile_of_all = pick_grad_tile(r, dim, piece, parts, want_x, form);   // the largest tiles take a length of which they fill the compute units
             for (int64_t p = piece; p >= piece / 2 && p >= 256; p -= up_to(piece / 32, 256)) {
-                if (pick_tile(p, dim, form) != tile_of_all) break;
+                if (pick_grad_tile(r, dim, p, parts, want_x, form) != tile_of_all) break;
                 const double t = (double)(n / p) * piece_cost(p, r, dim, parts, want_x, form) + (n % p ? piece_cost(up_to(n % p, 256), r, dim, parts, want_x, form) : 0);
                 if (t < least) { least = t; best = p; }
             }
@@ -1059,9 +1087,7 @@ struct GradPlan {
         // where few are multiplied at once the second product costs little
         two = dtype == AP_BF16 && r <= 128;
         c_part = r * ldc;
-        tile_c = pick_tile(piece, r, form);
-        tile = pick_tile(piece, dim, form);
-        if (tile > 128 && r <= 128) tile = 128;
+        tile = pick_grad_tile(r, dim, piece, two ? 2 : parts, want_x, form);
         runs = pick_runs(div_up(r, tile) * div_up(dim, tile), piece, div_up(piece, tile) * div_up(dim, tile), r, parts, tile, form);
         run_docs = (int32_t)up_to(div_up(piece, runs), 64);
         runs = (int32_t)div_up(piece, run_docs);
@@ -1089,13 +1115,13 @@ static int loss_pieces(const GradPlan &plan, ApLoss p, ApLossGrad g, int64_t n, 
         p.first = g.first = d0;
         p.count = g.count = (int32_t)std::min(plan.piece, n - d0);
         // a short last piece may take smaller tiles
-        AP_TRY((launch_tiles<OP, PARTS, true>(p, std::min(plan.tile_c, pick_tile(p.count, p.rows, plan.form)), st)));
-        const int tile = std::min(plan.tile, pick_tile(g.count, g.dim, plan.form));
-        const int64_t nt = div_up(g.dim, tile);
+        AP_TRY((launch_tiles<OP, PARTS, true>(p, pick_tile(p.count, p.rows, plan.form), st)));
         g.run_docs = plan.run_docs;
         g.start = d0 == 0;
         // a short last piece leaves the runs past its end alone
         g.runs = (uint32_t)(!g.gx ? 0 : g.start ? plan.runs : div_up(g.count, plan.run_docs));
+        const int tile = g.count == plan.piece || d0 == 0 ? plan.tile : pick_grad_tile(g.rows, g.dim, g.count, g.parts, g.runs > 0, plan.form, std::max<int64_t>(g.runs, 1));
+        const int64_t nt = div_up(g.dim, tile);
         const dim3 grid((unsigned)(g.runs * div_up(g.rows, tile) * nt + (g.grad_docs ? div_up(g.count, tile) * nt : 0)));
         if (tile == 64) hipLaunchKernelGGL((k_loss_grads<OP, 64, 64, 2, 2, PARTS>), grid, dim3(256), 0, st, g);
         else if constexpr (OP::BYTES == 2) {
