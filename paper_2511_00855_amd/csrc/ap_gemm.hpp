@@ -321,4 +321,12 @@ __device__ __forceinline__ void ap_g_tile(uint32_t block, uint32_t mt, uint32_t 
     *m = in / wide;
     *n = g * group + in % wide;
 }
+
+// What the tiles of m x n take, in rounds of the largest: one of 256 on every compute unit.  Two of 128 share one and take 0.74 of that time, four of 64 0.47; a round
+// that is not full takes half of one and its share (dispatch is even, but the last tiles run alone).
+static inline double ap_g_tiles_cost(int tile, int64_t m, int64_t n) {
+    const int64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), round = tile == 256 ? 256 : tile == 128 ? 512 : 1024, left = tiles % round;
+    if (tile == 256) return (double)((tiles + round - 1) / round);
+    return (tile == 128 ? 0.74 : 0.47) * ((double)(tiles / round) + (left ? 0.5 + 0.5 * (double)left / (double)round : 0.));
+}
 #endif

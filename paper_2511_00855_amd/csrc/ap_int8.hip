@@ -67,32 +67,32 @@ struct ApScores8 {
     int32_t group;
 };
 
-// Up to 32 queries: one pass over the documents, the queries in LDS.  Bound by its loads: 1,000,000 rows of 1,024 columns take 174 us for one query
+// Up to 16 queries: one pass over the documents, the queries in LDS.  Bound by its loads: 1,000,000 rows of 1,024 columns take 174 us for one query
 // (5.9 TB/s).
-template <int DT, int NQ>
+template <int DT>
 __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float s_scale[NQ * 16];
+    __shared__ float s_scale[16];
     const int lane = threadIdx.x & 63, wave = ap_wave_id();
     const int steps = (p.pad + 63) / 64;
-    for (int q = wave; q < NQ * 16; q += AP_STREAM_THREADS / 64) {
+    for (int q = wave; q < 16; q += AP_STREAM_THREADS / 64) {
         float s = 0.f;
         if (q < p.rows) {
             if (DT == AP_I8) {
                 for (int32_t c = lane * 4; c < steps * 64; c += 256)
-                    *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, NQ)) = c < p.pad ? *reinterpret_cast<const uint32_t *>(p.x + q * p.ldx + c) : 0u;
+                    *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, 1)) = c < p.pad ? *reinterpret_cast<const uint32_t *>(p.x + q * p.ldx + c) : 0u;
                 s = p.x_scale[q];
             } else {
-                s = round_row<DT == AP_I8 ? AP_F32 : DT>(p.x + q * p.ldx, p.dim, steps * 64, [&](int32_t c, uint32_t w) { *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, NQ)) = w; });
+                s = round_row<DT == AP_I8 ? AP_F32 : DT>(p.x + q * p.ldx, p.dim, steps * 64, [&](int32_t c, uint32_t w) { *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, 1)) = w; });
             }
         } else {
-            for (int32_t c = lane * 4; c < steps * 64; c += 256) *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, NQ)) = 0u;
+            for (int32_t c = lane * 4; c < steps * 64; c += 256) *reinterpret_cast<uint32_t *>(lds + ap_stream_place(q, c, 1)) = 0u;
         }
         if (lane == 0) s_scale[q] = s;
     }
     __syncthreads();
     struct Four { float v[4]; };
-    ap_stream<ApStreamI8, NQ>(p.q, p.ldq, p.n, p.pad, lds, (int64_t)blockIdx.x * (AP_STREAM_THREADS / 64) + wave, (int64_t)gridDim.x * (AP_STREAM_THREADS / 64),
+    ap_stream<ApStreamI8, 1>(p.q, p.ldq, p.n, p.pad, lds, (int64_t)blockIdx.x * (AP_STREAM_THREADS / 64) + wave, (int64_t)gridDim.x * (AP_STREAM_THREADS / 64),
                               [&](int64_t first) {
                                   const int64_t d = first + (lane >> 4) * 4;
                                   Four s;
@@ -100,16 +100,13 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) 
                                   for (int r = 0; r < 4; r++) s.v[r] = p.q_scale[d + r < p.n ? d + r : p.n - 1];
                                   return s;
                               },
-                              [&](int64_t first, const ap_g_i32x4 (&acc)[NQ], const Four &s) {
+                              [&](int64_t first, const ap_g_i32x4 (&acc)[1], const Four &s) {
                                   const int64_t d = first + (lane >> 4) * 4;
+                                  const int q = lane & 15;
+                                  if (q >= p.rows) return;
 #pragma unroll
-                                  for (int g = 0; g < NQ; g++) {
-                                      const int q = g * 16 + (lane & 15);
-                                      if (q >= p.rows) continue;
-#pragma unroll
-                                      for (int r = 0; r < 4; r++)
-                                          if (d + r < p.n) p.out[q * p.ld_out + d + r] = (float)acc[g][r] * s_scale[q] * s.v[r];
-                                  }
+                                  for (int r = 0; r < 4; r++)
+                                      if (d + r < p.n) p.out[q * p.ld_out + d + r] = (float)acc[0][r] * s_scale[q] * s.v[r];
                               });
 }
 
@@ -330,9 +327,9 @@ extern "C" int ap_quantize_rows(const void *x, int64_t ldx, int64_t rows, int32_
     return AP_OK;
 }
 
-// Up to how many queries one pass over the documents pays.  By one pass and by tiles, 16 queries: 33 and 53 us over 120,011 rows of 1,024 columns, 27 and 29 over
-// 100,000 of 768; 32: 44 and 50, 37 and 32, over 1,000,000 of 1,024 272 and 278.
-static bool scores8_few(int64_t rows, int32_t pad) { return rows <= 32 && ap_stream_lds(rows, pad) <= AP_STREAM_LDS; }
+// Up to how many queries one pass over the documents pays.  By one pass and by tiles, 16 queries: 34 and 35 us over 120,011 rows of 1,024 columns, 225 and 248 over
+// 1,000,000, 11 and 16 over 5,000 of 768; 32 (two groups of 16 in the pass): 43 and 37, 271 and 256, 16 and 17.
+static bool scores8_few(int64_t rows, int32_t pad) { return rows <= 16 && ap_stream_lds(rows, pad) <= AP_STREAM_LDS; }
 
 extern "C" int ap_scores_int8_bytes(int64_t rows, int32_t dim, int32_t x_dtype, size_t *out) {
     AP_REQUIRE(out != nullptr, "out is NULL");
@@ -344,16 +341,9 @@ extern "C" int ap_scores_int8_bytes(int64_t rows, int32_t dim, int32_t x_dtype, 
 }
 
 template <int DT> static int few(const ApScores8 &p, hipStream_t st) {
-    const int nq = (p.rows + 15) / 16;
     const size_t lds = (size_t)ap_stream_lds(p.rows, p.pad);
-    const dim3 grid((unsigned)ap_stream_blocks(p.n));
-#define AP_FEW(N)                                                                                                                       \
-    case N:                                                                                                                             \
-        if (lds > 60 * 1024) AP_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_scores8_few<DT, N>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
-        hipLaunchKernelGGL((k_scores8_few<DT, N>), grid, dim3(AP_STREAM_THREADS), lds, st, p);                                          \
-        break
-    switch (nq) { AP_FEW(1); AP_FEW(2); }
-#undef AP_FEW
+    if (lds > 60 * 1024) AP_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(k_scores8_few<DT>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_scores8_few<DT>), dim3((unsigned)ap_stream_blocks(p.n)), dim3(AP_STREAM_THREADS), lds, st, p);
     AP_CHECK_HIP(hipGetLastError());
     return AP_OK;
 }
@@ -382,8 +372,17 @@ extern "C" int ap_scores_int8(const void *x, int64_t ldx, const float *x_scale, 
         AP_TRY(ap_quantize_rows(x, ldx, rows, dim, x_dtype, qx, pad, sx, stream));
         p.x = reinterpret_cast<const char *>(qx); p.ldx = pad; p.x_scale = sx;
     }
+    // More than one round of the largest tiles: the one that takes the least (kernels and their launches: 64 queries over 120,011 rows of 1,024 columns 50, 46 and
+    // 38 us with 256, 128 and 64, 515 over 24,000 45, 35 and 44).  In one round all scores would leave at its end, so that smaller ones are better as long
+    // as they fill the compute units (500 over 20,000 of 384 28, 24 and 23 us), but not when three quarters of them have one of the largest (1,500 over
+    // 9,000 of 1,024 31, 39 and 44).
     int tile = 256;
-    while (tile > 64 && div_up(rows, tile) * div_up(n, tile) < 192) tile /= 2;
+    if (div_up(rows, 256) * div_up(n, 256) > 256) {
+        for (int t = 128; t >= 64; t /= 2)
+            if (ap_g_tiles_cost(t, rows, n) < ap_g_tiles_cost(tile, rows, n)) tile = t;
+    } else {
+        while (tile > 64 && div_up(rows, tile) * div_up(n, tile) < 192) tile /= 2;
+    }
     const int64_t tiles = div_up(rows, tile) * div_up(n, tile);
     AP_REQUIRE(tiles < (1ll << 31) / 512, "rows x n is too large");
     p.group = (int32_t)std::min<int64_t>(div_up(rows, tile), 8);

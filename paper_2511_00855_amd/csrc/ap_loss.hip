@@ -864,13 +864,6 @@ struct LossParts {   // f32 rows as two f16 parts
     }
 };
 
-// What the tiles of m x n take, in rounds of the largest: one of 256 on every compute unit.  Two of 128 share one and take 0.74 of that time, four of 64 0.47; a round
-// that is not full takes half of one and its share (dispatch is even, but the last tiles run alone).
-static double tiles_cost(int tile, int64_t m, int64_t n) {
-    const int64_t tiles = div_up(m, tile) * div_up(n, tile), round = tile == 256 ? 256 : tile == 128 ? 512 : 1024, left = tiles % round;
-    if (tile == 256) return (double)div_up(tiles, round);
-    return (tile == 128 ? 0.74 : 0.47) * ((double)(tiles / round) + (left ? 0.5 + 0.5 * (double)left / (double)round : 0.));
-}
 // The tile that takes the least; always 64 for the f32 instruction, which is so slow that small tiles cost it nothing and share the work out more evenly (a step of
 // 80 queries over 37,740 rows of 500: 256 us with tiles of 128, 190 with 64; 100 over 100,000 of 768 825 and 688; only a loss over 64,000 of 1,024
 // takes 139 us instead of 134).  bf16, kernel times with 256, 128 and 64: 515 queries over 24,000 rows of 1,024 53, 46 and 54 us; 1,500 over 9,000 33, 46 and 52;
@@ -879,7 +872,7 @@ static int pick_tile(int64_t m, int64_t n, LossForm form) {
     int best = 64;
     if (form != LOSS_F32)
         for (int t = 128; t <= 256; t *= 2)
-            if (tiles_cost(t, m, n) <= tiles_cost(best, m, n)) best = t;
+            if (ap_g_tiles_cost(t, m, n) <= ap_g_tiles_cost(best, m, n)) best = t;
     return best;
 }
 // The same for both gradients of a piece with the queries' in `runs` runs, in the lengths of k that a compute unit goes through.
@@ -1048,7 +1041,7 @@ struct GradPlan {
         const int64_t t = pick_grad_tile(r, dim, p, parts, want_x, form), more = div_up(p, t) * div_up(dim, t);
         int64_t least = div_up(more, 256) * (r * parts + 512);
         if (want_x) pick_runs(div_up(r, t) * div_up(dim, t), p, more, r, parts, (int)t, form, &least);
-        return tiles_cost(pick_tile(p, r, form), p, r) * (double)(dim * parts + 512) + (double)least * (t == 256 ? 1. : t == 128 ? 0.85 : 0.32) + 2 * 2048;   // two launches
+        return ap_g_tiles_cost(pick_tile(p, r, form), p, r) * (double)(dim * parts + 512) + (double)least * (t == 256 ? 1. : t == 128 ? 0.85 : 0.32) + 2 * 2048;   // two launches
     }
     size_t lay(char *base, int64_t rows, int64_t n, int32_t dim, int32_t dtype, bool want_x) {
         LossWs ws{base};
