@@ -92,6 +92,7 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) 
     }
     __syncthreads();
     struct Four { float v[4]; };
+    typedef float Out __attribute__((ext_vector_type(4), aligned(4)));
     ap_stream<ApStreamI8, 1>(p.q, p.ldq, p.n, p.pad, lds, (int64_t)blockIdx.x * (AP_STREAM_THREADS / 64) + wave, (int64_t)gridDim.x * (AP_STREAM_THREADS / 64),
                               [&](int64_t first) {
                                   const int64_t d = first + (lane >> 4) * 4;
@@ -104,9 +105,14 @@ __global__ __launch_bounds__(AP_STREAM_THREADS) void k_scores8_few(ApScores8 p) 
                                   const int64_t d = first + (lane >> 4) * 4;
                                   const int q = lane & 15;
                                   if (q >= p.rows) return;
+                                  float *to = p.out + q * p.ld_out + d;
+                                  Four v;
+#pragma unroll
+                                  for (int r = 0; r < 4; r++) v.v[r] = (float)acc[0][r] * s_scale[q] * s.v[r];
+                                  if (d + 3 < p.n) { *reinterpret_cast<Out *>(to) = Out{v.v[0], v.v[1], v.v[2], v.v[3]}; return; }
 #pragma unroll
                                   for (int r = 0; r < 4; r++)
-                                      if (d + r < p.n) p.out[q * p.ld_out + d + r] = (float)acc[0][r] * s_scale[q] * s.v[r];
+                                      if (d + r < p.n) to[r] = v.v[r];
                               });
 }
 
