@@ -814,7 +814,7 @@ extern "C" int ap_embed(const void *table, int64_t ld, int32_t dtype, int64_t vo
 // on, 13,400 entries of 384 take 35, 35 and 41 us in all, 32,000 of 768 51, 50 and 55, 250,000 of 128 in bf16 69, 66 and 67; 1.2M of 1,024 with runs of 64, 128
 // and 256 220, 229 and 228 for the runs and their joining.
 #define AP_RUN_LEAST 32
-#define AP_RUNS 65536
+#define AP_RUN_GROUPS 65536
 // Whether the rows that entries name are marked, so that zeros go to the others only: not where three quarters are others anyhow.  1.2M entries over 250,002 rows of
 // 2 KB: runs and zeros in one launch 234 us, all rows' zeros before the runs 277; 250,000 entries over 100,000: 168 and 186.
 #define AP_EMBED_NAMED(n, vocab) ((vocab) <= 4 * (n))
@@ -835,7 +835,7 @@ struct GradWs {
         bits = (int32_t)div_up(all, passes);
         blocks = div_up(n, AP_SORT_ITEMS(n));
         run = AP_RUN_LEAST;
-        while (run < 256 && n / run * div_up(dim, 64) > AP_RUNS) run *= 2;
+        while (run < 256 && n / run * div_up(dim, 64) > AP_RUN_GROUPS) run *= 2;
         runs = div_up(n, run);
         for (int i = 0; i < 2; i++) { sorted[i].of = (uint2 *)take(2 * n); sorted[i].w = (float *)take(n); }
         keys = (uint32_t *)take(n);
